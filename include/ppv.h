@@ -337,6 +337,82 @@ ppv_status ppv_topm_mask(const ppv_index_t *index, const int32_t *prefixes, int3
                          int32_t B, int32_t *top_ids, uint8_t *mask_V, uint32_t *mask, void *stream);
 
 /*
+ * ppv_token_logprobs -- log probabilities of tokens that are given: the scores of sequences that are there already (members of S under
+ * teacher forcing, sampled tokens), where constrained_sample draws new ones.  With l_v = logits[v] / T, p = softmax(l) and q = softmax(l)
+ * over the valid tokens alone (the distribution that constrained_sample draws from; q = p without a mask), per row b with token t:
+ *   logprobs[b]   = log q_t; -inf if t is not valid, not in [0, V), or has logit -inf
+ *   logZ_valid[b] = log sum_{v in mask} p_v (<= 0), as in constrained_sample; 0 without a mask.  logprobs + logZ_valid = log p_t, and their
+ *                   sums over a member's tokens are log P_L(a) and log x(a) of Algorithm 1
+ *   entropy[b]    = -sum_v q_v log q_v >= 0
+ *   stats[b]      what ppv_token_logprobs_backward needs of the row, PPV_LOGPROB_STATS words: a logit m, sum_v exp(l_v - m / T); a logit
+ *                 m' and the same over the valid tokens; the entropy; logprobs[b]; 0, 0
+ * A row without valid mass (an empty mask, or all valid tokens at -inf) has logZ_valid = -inf and entropy 0 (without a mask: a row
+ * of -inf alone).  A row whose token is negative (-1, what the sampling calls give where no token could be drawn; padding) is left out: its
+ * logits are not read and all its outputs are 0.
+ * Arguments (all device pointers):
+ *   logits, dt, row_stride, temperature   as in constrained_sample
+ *   mask      uint32[B, ceil(V/32)], or NULL: every token is valid
+ *   tokens    int32[B], or NULL: every row is taken and logprobs must be NULL
+ *   logprobs, logZ_valid, entropy   float[B] or NULL      stats  float[B, PPV_LOGPROB_STATS], 16-byte aligned, or NULL
+ * B == 0 is allowed and does nothing.  Errors: PPV_EINVAL (null logits, B < 0, V <= 0, row_stride < V or misaligned, bad dt or temperature,
+ * logprobs without tokens, no output at all, misaligned stats), PPV_ERANGE (V > PPV_MAX_VOCAB), PPV_EDEVICE.
+ */
+#define PPV_LOGPROB_STATS 8
+ppv_status ppv_token_logprobs(const void *logits, ppv_dtype dt, int64_t row_stride, const uint32_t *mask, const int32_t *tokens,
+                              int32_t B, int32_t V, float *logprobs, float *logZ_valid, float *entropy, float *stats,
+                              float temperature, void *stream);
+
+/*
+ * ppv_token_logprobs_backward -- the gradient of ppv_token_logprobs' outputs with respect to the logits.  With q, p as there and the
+ * upstream gradients g = d_logprobs[b], z = d_logZ_valid[b], h = d_entropy[b]:
+ *   d_logits[b, v] = (g (1[v = t] - q_v) + z (q_v - p_v) - h q_v (log q_v + entropy)) / T
+ * in fp32, rounded to dt once.  Without a mask logZ_valid is a constant and z counts for nothing.  A log probability of -inf is a constant
+ * too: its g counts for nothing.  A row without valid mass, and one that is left out, has a gradient of 0.
+ * Arguments (all device pointers):
+ *   logits, dt, row_stride, mask, tokens, temperature   as given to ppv_token_logprobs; tokens may be NULL where d_logprobs is
+ *   stats     float[B, PPV_LOGPROB_STATS], as ppv_token_logprobs left it for these arguments
+ *   d_logprobs, d_logZ_valid, d_entropy   float[B], or NULL: 0
+ *   d_logits  [B rows] of V elements of dt, written; d_row_stride and alignment as for the logits.  It may be the logits themselves (the
+ *             same address and stride), not overlap them otherwise.  What lies between the rows is not written.
+ * Errors: as ppv_token_logprobs; PPV_EINVAL also for null stats or d_logits, d_logprobs without tokens, an overlap.
+ */
+ppv_status ppv_token_logprobs_backward(const void *logits, ppv_dtype dt, int64_t row_stride, const uint32_t *mask, const int32_t *tokens,
+                                       const float *stats, const float *d_logprobs, const float *d_logZ_valid, const float *d_entropy,
+                                       int32_t B, int32_t V, void *d_logits, int64_t d_row_stride, float temperature, void *stream);
+
+/*
+ * ppv_token_logprobs_grad -- ppv_token_logprobs and ppv_token_logprobs_backward in one call, for training whose upstream gradients are
+ * known before the call (cross entropy: d_logprobs = -1 / rows; a policy gradient with given advantages): the row is read once where it
+ * can be held on the chip, and no statistics are kept.  Same arguments, same results up to the rounding of sums taken in another order.
+ *   logprobs, logZ_valid, entropy   float[B] or NULL (all may be)
+ * Errors: as the two calls.
+ */
+ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, int64_t row_stride, const uint32_t *mask, const int32_t *tokens,
+                                   const float *d_logprobs, const float *d_logZ_valid, const float *d_entropy, int32_t B, int32_t V,
+                                   float *logprobs, float *logZ_valid, float *entropy, void *d_logits, int64_t d_row_stride,
+                                   float temperature, void *stream);
+
+/*
+ * ppv_top_logprobs -- the k most probable valid tokens of a row with their log probabilities, and beside them what a server reports of
+ * the token it has drawn: its own log probability and the entropy.  q, T, tokens and left-out rows as in ppv_token_logprobs.
+ *   top_ids[b, i]       the row's i-th most probable valid token, i = 0 .. k-1; equal logits in increasing token id, -0 and +0 are equal;
+ *                       -1 where there are fewer than k (tokens at -inf are no alternatives)
+ *   top_logprobs[b, i]  its log q; -inf beside -1
+ *   logprobs, entropy   as in ppv_token_logprobs
+ * A row that is left out has top_ids -1 and top_logprobs -inf.  The ids of a row that holds NaN are -1 or inside [0, V) and otherwise
+ * unspecified.
+ * Arguments (all device pointers unless noted):
+ *   k         host, 1 .. PPV_TOP_MAX; may be more than V
+ *   top_ids   int32[B, k]      top_logprobs  float[B, k]      logprobs, entropy  float[B] or NULL
+ *   the others as in ppv_token_logprobs
+ * Errors: as ppv_token_logprobs; PPV_EINVAL also for k < 1, null top_ids or top_logprobs, PPV_ERANGE for k > PPV_TOP_MAX.
+ */
+#define PPV_TOP_MAX 128
+ppv_status ppv_top_logprobs(const void *logits, ppv_dtype dt, int64_t row_stride, const uint32_t *mask, const int32_t *tokens, int32_t B,
+                            int32_t V, int32_t k, int32_t *top_ids, float *top_logprobs, float *logprobs, float *entropy,
+                            float temperature, void *stream);
+
+/*
  * ppv_disc_select -- Algorithm 1 after SampleCandidate: a candidate is accepted with probability equal to its
  * importance score x, in at most K rounds, then importance resampling among K candidates with probability
  * x_k / sum x_k.  The candidates of all

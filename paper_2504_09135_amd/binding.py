@@ -25,12 +25,15 @@ PPV_MAX_VOCAB = 262144
 PPV_TOPM_MAX = 1024
 
 PPV_STATE_WORDS = 8
+PPV_LOGPROB_STATS = 8
+PPV_TOP_MAX = 128
 
 SYMBOLS = ("ppv_status_string", "ppv_build_index", "ppv_index_info", "ppv_index_export", "ppv_free_index",
            "ppv_index_save", "ppv_index_load",
            "ppv_next_token_mask", "constrained_sample", "ppv_decode_begin", "ppv_decode_step", "ppv_decode_loop", "ppv_topm_mask",
            "ppv_disc_select", "ppv_tuning_set", "ppv_tuning_get", "constrained_sample_noalloc",
-           "ppv_sample_next", "ppv_decode_begin_empty", "ppv_decode_first_step")
+           "ppv_sample_next", "ppv_decode_begin_empty", "ppv_decode_first_step",
+           "ppv_token_logprobs", "ppv_token_logprobs_backward", "ppv_token_logprobs_grad", "ppv_top_logprobs")
 PPV_NOALLOC_MAX_ROWS = 512
 
 # tuning / test switches (ppv_tuning_set)
@@ -92,6 +95,14 @@ def load_library() -> C.CDLL:
     lib.ppv_decode_loop.argtypes = [p, p, i32, p, p, p, p, C.c_int, i64, i64, p, i32, i32, p, p, p, C.c_float, p]
     lib.ppv_topm_mask.restype = C.c_int
     lib.ppv_topm_mask.argtypes = [p, p, i32, p, p, C.c_int, i64, i32, i32, p, p, p, p]
+    lib.ppv_token_logprobs.restype = C.c_int
+    lib.ppv_token_logprobs.argtypes = [p, C.c_int, i64, p, p, i32, i32, p, p, p, p, C.c_float, p]
+    lib.ppv_token_logprobs_backward.restype = C.c_int
+    lib.ppv_token_logprobs_backward.argtypes = [p, C.c_int, i64, p, p, p, p, p, p, i32, i32, p, i64, C.c_float, p]
+    lib.ppv_token_logprobs_grad.restype = C.c_int
+    lib.ppv_token_logprobs_grad.argtypes = [p, C.c_int, i64, p, p, p, p, p, i32, i32, p, p, p, p, i64, C.c_float, p]
+    lib.ppv_top_logprobs.restype = C.c_int
+    lib.ppv_top_logprobs.argtypes = [p, C.c_int, i64, p, p, i32, i32, i32, p, p, p, p, C.c_float, p]
     lib.ppv_disc_select.restype = C.c_int
     lib.ppv_disc_select.argtypes = [p, i32, i32, i32, p, p, i32, p, p, p, p]
     lib.ppv_tuning_set.restype = C.c_int
@@ -316,3 +327,49 @@ def ppv_sample_next(index: PPVIndex, prefixes: torch.Tensor, lens: torch.Tensor,
     st = (_call or _native()).sample_next(index, prefixes, lens, logits, uniforms, ids, logZ_valid, stream, temperature)
     if st:
         _check(st, "ppv_sample_next")
+
+
+def ppv_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, logprobs: Optional[torch.Tensor] = None,
+                       mask: Optional[torch.Tensor] = None, logZ_valid: Optional[torch.Tensor] = None,
+                       entropy: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None, stream=None,
+                       temperature: float = 1.0) -> None:
+    """Log probabilities of given tokens: logits [B, V] f32/bf16, tokens int32 [B] (negative: the row is left out), mask int32
+    [B, ceil(V/32)] or None -> logprobs, logZ_valid, entropy f32 [B], stats f32 [B, PPV_LOGPROB_STATS] (each optional)."""
+    st = (_call or _native()).token_logprobs(logits, mask, tokens, logprobs, logZ_valid, entropy, stats, stream, temperature)
+    if st:
+        _check(st, "ppv_token_logprobs")
+
+
+def ppv_token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Tensor], stats: torch.Tensor,
+                                d_logits: torch.Tensor, mask: Optional[torch.Tensor] = None,
+                                d_logprobs: Optional[torch.Tensor] = None, d_logZ_valid: Optional[torch.Tensor] = None,
+                                d_entropy: Optional[torch.Tensor] = None, stream=None, temperature: float = 1.0) -> None:
+    """The gradient of ppv_token_logprobs' outputs (upstream: d_logprobs, d_logZ_valid, d_entropy f32 [B], None: 0) with respect to
+    the logits, from the stats it left -> d_logits [B, V], of the logits' type (may be the logits themselves)."""
+    st = (_call or _native()).token_logprobs_backward(logits, mask, tokens, stats, d_logprobs, d_logZ_valid, d_entropy, d_logits,
+                                                      stream, temperature)
+    if st:
+        _check(st, "ppv_token_logprobs_backward")
+
+
+def ppv_token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], d_logits: torch.Tensor,
+                            logprobs: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                            d_logprobs: Optional[torch.Tensor] = None, d_logZ_valid: Optional[torch.Tensor] = None,
+                            d_entropy: Optional[torch.Tensor] = None, logZ_valid: Optional[torch.Tensor] = None,
+                            entropy: Optional[torch.Tensor] = None, stream=None, temperature: float = 1.0) -> None:
+    """ppv_token_logprobs and ppv_token_logprobs_backward in one call, for upstream gradients that are known before it."""
+    st = (_call or _native()).token_logprobs_grad(logits, mask, tokens, d_logprobs, d_logZ_valid, d_entropy, logprobs, logZ_valid,
+                                                  entropy, d_logits, stream, temperature)
+    if st:
+        _check(st, "ppv_token_logprobs_grad")
+
+
+def ppv_top_logprobs(logits: torch.Tensor, k: int, top_ids: torch.Tensor, top_logprobs: torch.Tensor,
+                     mask: Optional[torch.Tensor] = None, tokens: Optional[torch.Tensor] = None,
+                     logprobs: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None, stream=None,
+                     temperature: float = 1.0) -> None:
+    """The k most probable valid tokens of each row, most probable first: logits [B, V] f32/bf16, mask int32 [B, ceil(V/32)] or None
+    -> top_ids int32 [B, k], top_logprobs f32 [B, k]; with tokens int32 [B] also their logprobs f32 [B]; entropy f32 [B] (optional)."""
+    st = (_call or _native()).top_logprobs(logits, mask, tokens, k, top_ids, top_logprobs, logprobs, entropy, stream, temperature)
+    if st:
+        _check(st, "ppv_top_logprobs")

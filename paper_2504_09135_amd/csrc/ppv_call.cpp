@@ -12,6 +12,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -29,6 +30,10 @@ struct Entry {
     decltype(&::ppv_topm_mask) topm;
     decltype(&::ppv_disc_select) disc;
     decltype(&::ppv_sample_next) sample_next;
+    decltype(&::ppv_token_logprobs) token_logprobs;
+    decltype(&::ppv_token_logprobs_backward) token_logprobs_backward;
+    decltype(&::ppv_token_logprobs_grad) token_logprobs_grad;
+    decltype(&::ppv_top_logprobs) top_logprobs;
 } lib;
 
 PyObject *s_handle, *s_n_words, *s_vocab, *s_cuda_stream;   // interned attribute names
@@ -140,10 +145,10 @@ struct Logits {
     ppv_dtype dtype;
     int64_t row_stride;
     int64_t B, V;
-    explicit Logits(PyObject *o) {
-        const at::Tensor &t = tensor(o, "logits");
+    explicit Logits(PyObject *o, const char *name = "logits") {
+        const at::Tensor &t = tensor(o, name);
         if (t.dim() != 2 || !t.is_cuda() || t.stride(1) != 1)
-            raise(PyExc_ValueError, "logits: need a 2-D GPU tensor with unit stride along the vocabulary");
+            raise(PyExc_ValueError, "%s: need a 2-D GPU tensor with unit stride along the vocabulary", name);
         dtype = logits_dtype(t);
         B = t.size(0);
         V = t.size(1);
@@ -389,6 +394,105 @@ PyObject *sample_next(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// What the calls on given tokens share: the rows' optional arguments have the shape [B] and lie on the logits' device, which is the current
+// one for the call and its stream.
+struct Rows {
+    const char *call;
+    Logits l;
+    c10::hip::HIPGuard device;
+    Rows(const char *name, PyObject *logits) : call(name), l(logits), device((c10::DeviceIndex)THPVariable_Unpack(logits).get_device()) {
+        if (l.B > INT32_MAX || l.V > INT32_MAX) raise(PyExc_ValueError, "%s: too many logits", name);
+    }
+    void here(const Arg &x) const {
+        if (!x.none() && tensor(x.o, x.name).is_cuda() && tensor(x.o, x.name).get_device() != device.current_device().index())
+            raise(PyExc_ValueError, "%s: %s is on another device than the logits", call, x.name);
+    }
+    template <typename P> P *get(const Arg &x, at::ScalarType dtype, int64_t m = -1) const {
+        if (!x.fits_or_none(l.B, m)) raise(PyExc_ValueError, m < 0 ? "%s: %s must have shape [B]" : "%s: %s has the wrong shape", call, x.name);
+        here(x);
+        return x.get<P>(dtype);
+    }
+    const uint32_t *mask(PyObject *o) const { return get<uint32_t>(Arg{o, "mask"}, I32, (l.V + 31) / 32); }
+    const int32_t *tokens(PyObject *o) const { return get<int32_t>(Arg{o, "tokens"}, I32); }
+    float *f32(PyObject *o, const char *name, int64_t m = -1) const { return get<float>(Arg{o, name}, F32, m); }
+    Logits gradient(PyObject *o) const {   // rows like the logits'
+        const Logits d(o, "d_logits");
+        if (d.B != l.B || d.V != l.V || d.dtype != l.dtype) raise(PyExc_ValueError, "%s: d_logits must have the logits' shape and type", call);
+        here(Arg{o, "d_logits"});
+        return d;
+    }
+};
+
+// logits, mask, tokens, logprobs, logZ_valid, entropy, stats, stream, temperature
+PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded("token_logprobs", n, 9, [&] {
+        const Rows r("ppv_token_logprobs", a[0]);
+        const uint32_t *mk = r.mask(a[1]);
+        const int32_t *tk = r.tokens(a[2]);
+        float *lp = r.f32(a[3], "logprobs"), *zv = r.f32(a[4], "logZ_valid"), *h = r.f32(a[5], "entropy"),
+              *st = r.f32(a[6], "stats", PPV_LOGPROB_STATS);
+        const float T = temperature_of(a[8]);
+        void *s = stream_of(a[7]);
+        return status([&] {
+            return lib.token_logprobs(r.l.ptr, r.l.dtype, r.l.row_stride, mk, tk, (int32_t)r.l.B, (int32_t)r.l.V, lp, zv, h, st, T, s);
+        });
+    });
+}
+
+// logits, mask, tokens, stats, d_logprobs, d_logZ_valid, d_entropy, d_logits, stream, temperature
+PyObject *token_logprobs_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded("token_logprobs_backward", n, 10, [&] {
+        const Rows r("ppv_token_logprobs_backward", a[0]);
+        const uint32_t *mk = r.mask(a[1]);
+        const int32_t *tk = r.tokens(a[2]);
+        const float *st = r.f32(a[3], "stats", PPV_LOGPROB_STATS), *g = r.f32(a[4], "d_logprobs"), *z = r.f32(a[5], "d_logZ_valid"),
+                    *h = r.f32(a[6], "d_entropy");
+        const Logits d = r.gradient(a[7]);
+        const float T = temperature_of(a[9]);
+        void *s = stream_of(a[8]);
+        return status([&] {
+            return lib.token_logprobs_backward(r.l.ptr, r.l.dtype, r.l.row_stride, mk, tk, st, g, z, h, (int32_t)r.l.B, (int32_t)r.l.V,
+                                               (void *)d.ptr, d.row_stride, T, s);
+        });
+    });
+}
+
+// logits, mask, tokens, d_logprobs, d_logZ_valid, d_entropy, logprobs, logZ_valid, entropy, d_logits, stream, temperature
+PyObject *token_logprobs_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded("token_logprobs_grad", n, 12, [&] {
+        const Rows r("ppv_token_logprobs_grad", a[0]);
+        const uint32_t *mk = r.mask(a[1]);
+        const int32_t *tk = r.tokens(a[2]);
+        const float *g = r.f32(a[3], "d_logprobs"), *z = r.f32(a[4], "d_logZ_valid"), *h = r.f32(a[5], "d_entropy");
+        float *lp = r.f32(a[6], "logprobs"), *zv = r.f32(a[7], "logZ_valid"), *en = r.f32(a[8], "entropy");
+        const Logits d = r.gradient(a[9]);
+        const float T = temperature_of(a[11]);
+        void *s = stream_of(a[10]);
+        return status([&] {
+            return lib.token_logprobs_grad(r.l.ptr, r.l.dtype, r.l.row_stride, mk, tk, g, z, h, (int32_t)r.l.B, (int32_t)r.l.V, lp, zv, en,
+                                           (void *)d.ptr, d.row_stride, T, s);
+        });
+    });
+}
+
+// logits, mask, tokens, k, top_ids, top_logprobs, logprobs, entropy, stream, temperature
+PyObject *top_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded("top_logprobs", n, 10, [&] {
+        const Rows r("ppv_top_logprobs", a[0]);
+        const uint32_t *mk = r.mask(a[1]);
+        const int32_t *tk = r.tokens(a[2]);
+        const int64_t k = int_of(a[3]);
+        if (k > INT32_MAX || k < INT32_MIN) raise(PyExc_ValueError, "ppv_top_logprobs: k is out of range");
+        int32_t *ids = r.get<int32_t>(Arg{a[4], "top_ids"}, I32, k < 0 ? 0 : k);
+        float *tl = r.f32(a[5], "top_logprobs", k < 0 ? 0 : k), *lp = r.f32(a[6], "logprobs"), *h = r.f32(a[7], "entropy");
+        const float T = temperature_of(a[9]);
+        void *s = stream_of(a[8]);
+        return status([&] {
+            return lib.top_logprobs(r.l.ptr, r.l.dtype, r.l.row_stride, mk, tk, (int32_t)r.l.B, (int32_t)r.l.V, (int32_t)k, ids, tl, lp, h, T, s);
+        });
+    });
+}
+
 // bind({entry point's name: its address})
 PyObject *bind(PyObject *, PyObject *table) {
     if (!PyDict_Check(table)) return PyErr_Format(PyExc_TypeError, "bind: need a dict of addresses");
@@ -414,6 +518,10 @@ PyObject *bind(PyObject *, PyObject *table) {
     e.topm = (decltype(e.topm))find("ppv_topm_mask");
     e.disc = (decltype(e.disc))find("ppv_disc_select");
     e.sample_next = (decltype(e.sample_next))find("ppv_sample_next");
+    e.token_logprobs = (decltype(e.token_logprobs))find("ppv_token_logprobs");
+    e.token_logprobs_backward = (decltype(e.token_logprobs_backward))find("ppv_token_logprobs_backward");
+    e.token_logprobs_grad = (decltype(e.token_logprobs_grad))find("ppv_token_logprobs_grad");
+    e.top_logprobs = (decltype(e.top_logprobs))find("ppv_top_logprobs");
     if (!fine) return nullptr;
     lib = e;
     Py_RETURN_NONE;
@@ -422,7 +530,8 @@ PyObject *bind(PyObject *, PyObject *table) {
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(next_token_mask), FAST(sample),      FAST(decode_begin), FAST(decode_begin_empty),
                          FAST(decode_step),     FAST(decode_loop), FAST(topm_mask),    FAST(disc_select),
-                         FAST(sample_next),     {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         FAST(sample_next),     FAST(token_logprobs), FAST(token_logprobs_backward), FAST(token_logprobs_grad),
+                         FAST(top_logprobs),    {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ppv_call", "Native argument checks and calls of binding.py.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

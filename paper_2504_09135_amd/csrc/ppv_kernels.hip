@@ -22,6 +22,7 @@
 
 #include "ppv_device.h"
 #include "ppv_internal.h"
+#include "ppv_rows.h"
 #include "ppv_walk.h"
 
 namespace {
@@ -30,21 +31,9 @@ constexpr int MASK_THREADS = 256;
 constexpr int MAX_WAVES = 16;                 // wavefronts per row (workgroup of up to 1024 threads)
 constexpr int LOOP_WAVES = 8;                 // the decode-loop kernel with the list in LDS
 constexpr int MAX_TILES = PPV_MAX_TILES;
-constexpr float LN2F = 0.693147180559945309417f;
 static_assert(PPV_MAX_VOCAB <= MAX_TILES * 1024, "tile bookkeeping too small");
 
-__device__ __forceinline__ float fast_exp2(float y) { return __builtin_amdgcn_exp2f(y); }  // v_exp_f32, 1 ulp
-__device__ __forceinline__ float fast_log2(float y) { return __builtin_amdgcn_logf(y); }   // v_log_f32, 1 ulp (normal inputs)
 // exp(d) for d <= 0 with the rounding of d*log2(e) compensated (used once per tile, not per token)
-// Temperature (Algorithm 1's input T): P = softmax(logits / T).  The division is folded into the constant of the
-// exponentials, c = log2(e) / T, so that it costs nothing per token; differences of logits that enter a result
-// as they are (a reference minus another) are multiplied by inv = 1 / T.  T = 1 gives c = log2(e), inv = 1.
-struct Temper {
-    float c;
-    float inv;
-    float guard;   // how far above an image tile's reference a logit may lie (REF_GUARD * T, see image_stats)
-};
-
 __device__ __forceinline__ float exp_scale(float d, float c) {
     float hi = d * c;
     float lo = fmaf(d, c, -hi);
@@ -177,117 +166,6 @@ __global__ __launch_bounds__(MASK_THREADS) void mask_rows_kernel(const int32_t *
     if (lane < n_words) mask[(size_t)b * (size_t)n_words + lane] = word;
 }
 
-// ------------------------------------------------------------------------------------------
-// Tiles.  A tile is what one wavefront loads with four 16-byte loads per lane: 2048 bf16 or 1024
-// fp32 tokens.  Load j of lane l holds the EPL consecutive tokens starting at
-// tile*TILE + j*64*EPL + l*EPL, so token order inside a tile is (j, lane, k).
-template <typename T> struct Elem;
-template <> struct Elem<float> {
-    static constexpr int EPL = 4;  // tokens per 16-byte load
-    __device__ static __forceinline__ void unpack(const u32x4 &r, float x[4]) {
-        x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y);
-        x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
-    }
-};
-template <> struct Elem<uint16_t> {  // bf16: widening to fp32 is exact
-    static constexpr int EPL = 8;
-    __device__ static __forceinline__ void unpack(const u32x4 &r, float x[8]) {
-        x[0] = __uint_as_float(r.x << 16); x[1] = __uint_as_float(r.x & 0xFFFF0000u);
-        x[2] = __uint_as_float(r.y << 16); x[3] = __uint_as_float(r.y & 0xFFFF0000u);
-        x[4] = __uint_as_float(r.z << 16); x[5] = __uint_as_float(r.z & 0xFFFF0000u);
-        x[6] = __uint_as_float(r.w << 16); x[7] = __uint_as_float(r.w & 0xFFFF0000u);
-    }
-};
-// The same as unpack, with values that the compiler takes for new ones each time: what is unpacked is used at once and
-// not kept in registers for another use of the tile (there is one in a rare case, and tiles are held packed).
-template <typename T> __device__ __forceinline__ void unpack_fresh(const u32x4 &r, float x[Elem<T>::EPL]) {
-    if (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) x[i] = __uint_as_float(r[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            asm volatile("v_lshlrev_b32 %0, 16, %1" : "=v"(x[(2 * i) % Elem<T>::EPL]) : "v"(r[i]));
-            asm volatile("v_and_b32 %0, %2, %1" : "=v"(x[(2 * i + 1) % Elem<T>::EPL]) : "v"(r[i]), "s"(0xFFFF0000u));
-        }
-    }
-}
-template <typename T> struct TileGeom {
-    static constexpr int EPL = Elem<T>::EPL;
-    static constexpr int PER_LOAD = WAVE * EPL;   // tokens covered by one load of the wave
-    static constexpr int TILE = 4 * PER_LOAD;     // tokens per tile
-    static constexpr int WORDS = TILE / 32;       // mask words per tile
-    static constexpr int LANES_PER_WORD = 32 / EPL;
-};
-
-struct RawTile {
-    u32x4 r[4];
-    uint32_t word;   // image path: this lane's word of the tile's mask (requested together with the tile)
-};
-
-// A tile is requested with four unconditional 16-byte loads wherever it lies, also at the row's end and behind it; group_of puts
-// -inf behind the end when the tile is used.  Nothing is conditional between request and use, so the compiler can
-// count the loads in flight and wait for exactly the ones a use needs, and the ragged last tile is one like the others.
-// One addition makes the four addresses (clamped into the row by comparisons, as here before, they took twelve).
-template <typename T>
-__device__ __forceinline__ void load_tile(const Row &row, int tile, int lane, RawTile &rt) {
-    const uint32_t at = (uint32_t)tile * (4 * WAVE * 16u) + (uint32_t)lane * 16u;
-#pragma unroll
-    for (int j = 0; j < 4; j++) rt.r[j] = __builtin_amdgcn_raw_buffer_load_b128(row.buf, at + j * (WAVE * 16u), 0, 2 /* non-temporal */);
-}
-constexpr int NO_TILE = 1 << 18;   // behind every row: a request that reads nothing
-// The tile's tokens that lie inside the row, counted from this lane's first one (PAD: what is behind the row's end counts
-// as -inf; only the row's last tile has any of that).
-template <typename T> __device__ __forceinline__ int tokens_left(int V, int tile, int lane) {
-    return V - tile * TileGeom<T>::TILE - lane * TileGeom<T>::EPL;
-}
-// group j of a tile, unpacked
-template <typename T, bool PAD> __device__ __forceinline__ void group_of(const RawTile &rt, int j, int left, float x[TileGeom<T>::EPL]) {
-    unpack_fresh<T>(rt.r[j], x);
-    if (PAD) {
-        int in = left - j * TileGeom<T>::PER_LOAD;
-        asm("" : "+v"(in));   // (or the compiler compares `left` with a constant for each token, each in a register of its own)
-#pragma unroll
-        for (int k = 0; k < TileGeom<T>::EPL; k++) x[k] = k < in ? x[k] : -INFINITY;
-    }
-}
-
-// word wi of a V-bit image, with bits at positions >= V cleared (0 beyond the image), in two parts: the load, unconditional
-// (clamped index: a conditional load would make later waits conservative), and what is done to the word once it is
-// used (at the load it would wait for it, and for every tile asked for before).
-__device__ __forceinline__ uint32_t image_word_raw(const uint32_t *__restrict__ image, int wi, int V) {
-    const int last = (V + 31) / 32 - 1;
-    return image[wi < last ? wi : last];
-}
-__device__ __forceinline__ uint32_t image_word_fix(uint32_t w, int wi, int V) {
-    const int last = (V + 31) / 32 - 1;
-    if (wi == last && (V & 31)) w &= (1u << (V & 31)) - 1u;
-    return wi <= last ? w : 0u;
-}
-__device__ __forceinline__ uint32_t image_word(const uint32_t *__restrict__ image, int wi, int V) {
-    return image_word_fix(image_word_raw(image, wi, V), wi, V);
-}
-// the tile's mask word for this lane (lane l < WORDS holds word l of the tile), in the same two parts
-template <typename T> __device__ __forceinline__ uint32_t tile_word_raw(const uint32_t *__restrict__ image, int tile, int lane, int V) {
-    using G = TileGeom<T>;
-    return image_word_raw(image, tile * G::WORDS + (lane < G::WORDS ? lane : 0), V);
-}
-template <typename T> __device__ __forceinline__ uint32_t tile_word_fix(uint32_t w, int tile, int lane, int V) {
-    using G = TileGeom<T>;
-    return lane < G::WORDS ? image_word_fix(w, tile * G::WORDS + lane, V) : 0u;
-}
-template <typename T>
-__device__ __forceinline__ uint32_t tile_mask_word(const uint32_t *__restrict__ image, int tile, int lane, int V) {
-    return tile_word_fix<T>(tile_word_raw<T>(image, tile, lane, V), tile, lane, V);
-}
-
-// mask bits of this lane's EPL tokens of load j, from the tile's mask words (lane l < WORDS holds word l)
-template <typename T> __device__ __forceinline__ uint32_t lane_bits(uint32_t tile_word, int j, int lane) {
-    using G = TileGeom<T>;
-    uint32_t w = (uint32_t)__shfl((int)tile_word, j * (G::WORDS / 4) + lane / G::LANES_PER_WORD, WAVE);
-    return (w >> ((lane % G::LANES_PER_WORD) * G::EPL)) & ((1u << G::EPL) - 1u);
-}
-
 // References far from 0.  With |m*c| of 2^31 and more the rounding of m*c is beyond the range of exp2, and a product with a
 // stand-in for -inf (the type's lowest number, -1e30) is outside fp32.  An exact maximum is therefore taken no lower than
 // m*c = -FAR (far tokens weigh nothing against that).  Where a whole row, or its largest token, lies beyond that on either side, the
@@ -339,7 +217,6 @@ __device__ __forceinline__ Shifted shifted(float m, float c) {
 // The second copy of the sums for tiles that are summed again stands out of the way of the first.  Tiles that were set aside
 // and loaded once more behind the others took filtered rows up to twice as long (constrained_sample, 50 tokens left of
 // V = 32k, 2,048 rows: 47.5 us against 25.3; V = 50k fp32, 384 rows: 29.8 against 16.4).
-constexpr float REF_GUARD = 40.f;   // exp(40) * 2048 tokens is far inside fp32
 constexpr float SUM_MOST = 2.353852668e17f;   // exp(REF_GUARD)
 constexpr float REF_LOW = -5e3f;
 // (as unsigned numbers, negative floats grow with their size, and infinities and NaNs are above the other positive ones)
@@ -2249,24 +2126,6 @@ __global__ __launch_bounds__((LOOP && !REG ? LOOP_WAVES : MAX_WAVES) * WAVE, LOO
         if (logx) logx[b] = lx;
         if (done) active[b] = 0;
     }
-}
-
-// T > 0 and finite, or the call is refused; the constants the kernels take (see Temper)
-bool temper_for(float temperature, Temper *tp) {
-    if (!(temperature > 0.f) || !std::isfinite(temperature)) return false;
-    tp->c = (float)(1.44269504088896340736 / (double)temperature);   // log2(e) / T
-    tp->inv = (float)(1.0 / (double)temperature);
-    tp->guard = REF_GUARD * temperature;
-    return std::isfinite(tp->c) && tp->c > 0.f;
-}
-
-ppv_status check_logits_args(const void *logits, ppv_dtype dt, int64_t row_stride, int32_t V) {
-    if (!logits || V <= 0 || row_stride < V) return PPV_EINVAL;
-    if (dt != PPV_F32 && dt != PPV_BF16) return PPV_EINVAL;
-    const int64_t per16 = (dt == PPV_F32) ? 4 : 8;
-    if (row_stride % per16 != 0 || ((uintptr_t)logits & 15u) != 0) return PPV_EINVAL;
-    if (V > PPV_MAX_VOCAB) return PPV_ERANGE;
-    return PPV_OK;
 }
 
 // Wavefronts per row: a power of two, at most one per tile and at most MAX_WAVES.  A small batch is
