@@ -6,9 +6,8 @@
 //   log Z_valid    = log sum_valid e^l - log sum e^l
 //   entropy        = -sum q log q = log S - (sum y e^y) / S       with y = l - reference, S = sum e^y over the valid tokens
 //   d_l            = d_logprob (1[v = t] - q) + d_logZ (q - p) - d_entropy q (log q + entropy),   d_logits = d_l / T
-// A row is read once, by all lanes of its wavefronts, each with its own running reference (the largest logit it has seen) and sums
-// relative to it; the lanes' sums are brought to one reference at the end.  Differences of logits are taken before they are
-// multiplied, so that rows far from 0 lose nothing.  Sums are fp32: a lane adds at most 4,096 terms of one sign.
+// A row is read once, by all lanes of its wavefronts, each with its own running reference and sums relative to it; the lanes' sums are
+// brought to one reference at the end.  Sums are fp32: a lane adds at most 4,096 terms of one sign.
 #include "ppv_rows.h"
 
 namespace {
@@ -19,13 +18,6 @@ constexpr unsigned MOST_GROUPS = 1u << 20;   // workgroups of a launch: more row
 constexpr float LOWEST = -3.402823466e38f;
 constexpr float FAINT = -1000.f;     // as an exponent of 2: a weight of 0
 
-// ------------------------------------------------------------------------------------------
-// Sums over tokens: reference m, s = sum 2^((x - m) c), w = sum of each of these times its exponent.  An empty sum has m = LOWEST, which
-// is finite: no difference below is that of two infinities.
-struct Sums {
-    float m, s, w;
-};
-__device__ __forceinline__ Sums no_sums() { return {LOWEST, 0.f, 0.f}; }
 __device__ __forceinline__ float most(float a, float b) {   // (without the instruction that quiets a NaN first)
     float r;
     asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
@@ -36,30 +28,135 @@ __device__ __forceinline__ float most(float a, float b, float c) {
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
-// sums relative to the reference m, which is not below their own
-template <bool W> __device__ __forceinline__ void refer(Sums &a, float m, float c) {
-    const float d = most((a.m - m) * c, FAINT), f = fast_exp2(d);
-    if (W) a.w = f * fmaf(d, a.s, a.w);
-    a.s *= f;
-    a.m = m;
-}
-template <int N, bool W> __device__ __forceinline__ void take(Sums &a, const float (&x)[N], float c) {
-    float m = a.m;
+template <int N> __device__ __forceinline__ float most_of(const float (&x)[N], float so_far) {
+    float m = so_far;
 #pragma unroll
     for (int i = 0; i < N; i += 2) m = most(m, x[i], x[i + 1]);
-    refer<W>(a, m, c);
+    return m;
+}
+__device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
+
+// ------------------------------------------------------------------------------------------
+// Sums over tokens, in two forms.
+//   Run    s = sum 2^(x c - r), w = sum of each of these times its exponent: one multiply-add and an exponential a token.  Any r gives the
+//          same sums as long as they stay inside fp32, so a lane's r is the first group's largest token and is raised only where one
+//          lies RAISE above it: a comparison a group.  (x c is not rounded before r is taken from it, and r is a reference of its own, no logit's.)
+//          r is no lower than -FAR_OFF: a caller's stand-in for -inf (the type's lowest number, -1e30) weighs nothing, and the sum of
+//          nothing else is 0.  Rows beyond FAR_OFF, to either side, are seen by that or by their largest token, and summed again in the
+//          careful form.
+//   Sums   s = sum 2^((x - m) c): the difference first, exact for an x within a factor of 2 of m; the reference is the largest token.
+// An empty sum has a reference of LOWEST, which is finite: no difference below is that of two infinities.
+constexpr float FAR_OFF = 134217728.f;   // 2^27: below it the rounding of r is at most four units of the exponent
+constexpr float RAISE = 12.f;            // units of the exponent; entropies lose 12 * 2^-24 where a row's largest token comes late
+constexpr float FAINT_SUM = 9.09494702e-13f;   // 2^-40: valid tokens that weigh less than that against the lane's reference get one of their own
+constexpr float LOSES = -40.f;
+struct Run {
+    float r, s, w;
+};
+struct Sums {
+    float m, s, w;
+};
+__device__ __forceinline__ Run no_run() { return {-FAR_OFF, 0.f, 0.f}; }
+__device__ __forceinline__ Sums no_sums() { return {LOWEST, 0.f, 0.f}; }
+
+// A lane's share of a row.
+struct Tally {
+    Run all;            // over all tokens (W without a mask: with w)
+    float top, limit;   // the largest token; one above `limit` raises the reference
+    float s, w;         // with a mask: the valid tokens relative to all.r ...
+    Run few;            // ... and relative to a reference of their own
+    float few_top, few_limit;
+    uint32_t seen;      // bits of the mask
+};
+__device__ __forceinline__ Tally no_tally() { return {no_run(), -INFINITY, LOWEST, 0.f, 0.f, no_run(), -INFINITY, LOWEST, 0u}; }
+__device__ __forceinline__ void refer(float &s, float &w, float d) {   // to a reference that lies -d above
+    const float f = fast_exp2(d);
+    w = f * fmaf(d, s, w);
+    s *= f;
+}
+__device__ __forceinline__ float reference_at(float top, float c) { return most(top * c, -FAR_OFF); }
+template <bool W> __device__ __forceinline__ Run both(const Run &a, const Run &b) {
+    const float ra = a.s != 0.f ? a.r : LOWEST, rb = b.s != 0.f ? b.r : LOWEST, R = most(ra, rb);
+    const float da = most(ra - R, FAINT), db = most(rb - R, FAINT), fa = fast_exp2(da), fb = fast_exp2(db);
+    return {R, fa * a.s + fb * b.s, W ? fa * fmaf(da, a.s, a.w) + fb * fmaf(db, b.s, b.w) : 0.f};
+}
+// The lane's reference is raised to its largest token where that lies above the limit (lanes whose does not: nothing changes).
+template <bool MASK> __device__ __forceinline__ void raise(Tally &a, float c, float step) {
+    if (__ballot(a.top > a.limit) == 0ull) return;
+    const bool up = a.top > a.limit;
+    const float r = up ? reference_at(a.top, c) : a.all.r, d = a.all.r - r;
+    if (MASK && a.s != 0.f && d < LOSES) {   // the valid tokens so far would vanish against the new one
+        a.few = both<true>(a.few, {a.all.r, a.s, a.w});
+        a.few_limit = fmaf(a.few.r, __builtin_amdgcn_rcpf(c), step);
+        a.s = a.w = 0.f;
+    }
+    refer(a.all.s, a.all.w, d);
+    if (MASK) refer(a.s, a.w, d);
+    a.all.r = r;
+    a.limit = up ? a.top + step : a.limit;
+}
+template <int N, bool W> __device__ __forceinline__ void add(Run &a, const float (&x)[N], float c) {
 #pragma unroll
     for (int i = 0; i < N; i++) {
-        const float y = (x[i] - m) * c, e = fast_exp2(y);
+        const float y = fmaf(x[i], c, -a.r), e = fast_exp2(y);
         a.s += e;
         if (W) a.w = fmaf(most(y, FAINT), e, a.w);   // (-inf: nothing, not a NaN)
     }
 }
-template <bool W> __device__ __forceinline__ Sums over_wave(Sums a, float c) {
-    refer<W>(a, wave_max(a.m), c);
-    a.s = wave_sum(a.s);
-    if (W) a.w = wave_sum(a.w);
-    return a;
+__device__ __forceinline__ float if_bit(float x, uint32_t bits, int k) { return (bits >> k) & 1u ? x : -INFINITY; }
+// A group of a lane's tokens, `bits`: the valid ones.  Where few lanes have any, those are summed by themselves; else with the exponentials
+// that are there, unless a lane's weigh too little against its reference for that.
+constexpr int FEW_LANES = 12;
+template <int N, bool MASK, bool W> __device__ __forceinline__ void take_group(Tally &a, float (&x)[N], uint32_t bits, float c, float step) {
+    a.top = most_of<N>(x, a.top);
+    raise<MASK>(a, c, step);
+    if (!MASK) {
+        add<N, W>(a.all, x, c);
+        return;
+    }
+    const uint64_t lanes = __ballot(bits != 0u);
+    bool alone = bits != 0u;
+    if (__popcll(lanes) <= FEW_LANES) {
+        add<N, false>(a.all, x, c);
+        if (lanes == 0ull) return;
+    } else {
+        float s = 0.f, w = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const float y = fmaf(x[i], c, -a.all.r), e = fast_exp2(y);
+            a.all.s += e;
+            const float v = __uint_as_float(__float_as_uint(e) & (uint32_t)((int32_t)(bits << (31 - i)) >> 31));
+            s += v;
+            if (W) w = fmaf(most(y, FAINT), v, w);
+        }
+        alone = alone && s < FAINT_SUM;
+        a.s += alone ? 0.f : s;
+        if (W) a.w += alone ? 0.f : w;
+        if (__ballot(alone) == 0ull) return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++) x[i] = if_bit(x[i], alone ? bits : 0u, i);
+    a.few_top = most_of<N>(x, a.few_top);
+    if (a.few_top > a.few_limit) {
+        const float r = reference_at(a.few_top, c);
+        refer(a.few.s, a.few.w, a.few.r - r);
+        a.few.r = r;
+        a.few_limit = a.few_top + step;
+    }
+    add<N, W>(a.few, x, c);
+}
+
+template <typename T> __device__ __forceinline__ int tiles_in(int V) { return (V + TileGeom<T>::TILE - 1) / TileGeom<T>::TILE; }
+
+template <bool W> __device__ __forceinline__ Run over_lanes(const Run &a) {   // the wavefront's
+    const float r = a.s != 0.f ? a.r : LOWEST, R = wave_max(r), d = most(r - R, FAINT), f = fast_exp2(d);
+    return {R, wave_sum(f * a.s), W ? wave_sum(f * fmaf(d, a.s, a.w)) : 0.f};
+}
+// relative to a logit that makes the sum about 1: weights are then no smaller against it than they are
+__device__ __forceinline__ Sums sums_of(const Run &a, float c) {
+    if (!(a.s != 0.f)) return no_sums();
+    const float m = (a.r + fast_log2(a.s)) * __builtin_amdgcn_rcpf(c), d = fmaf(-m, c, a.r), f = fast_exp2(d);
+    return {m, f * a.s, f * fmaf(d, a.s, a.w)};
 }
 
 // A row's mask as the memory unit's buffer; what is asked for behind its end is 0.
@@ -74,68 +171,157 @@ template <typename T> __device__ __forceinline__ uint32_t bits_raw(const Row &ma
 template <typename T> __device__ __forceinline__ uint32_t bits_fix(uint32_t raw, int lane) {
     return TileGeom<T>::EPL == 8 ? raw : (raw >> ((lane & 1) * 4)) & 0xFu;
 }
-__device__ __forceinline__ float if_bit(float x, uint32_t bits, int k) { return (bits >> k) & 1u ? x : -INFINITY; }
-
-template <typename T> struct MaskedTile {
+template <typename T, bool MASK> struct MaskedTile {
     RawTile t;
     uint32_t bits[4];
-    template <bool MASK> __device__ __forceinline__ void load(const Row &row, const Row &mask, int tile, int lane) {
+    __device__ __forceinline__ void load(const Row &row, const Row &mask, int tile, int lane) {
         load_tile<T>(row, tile, lane, t);
         if (MASK) {
 #pragma unroll
             for (int j = 0; j < 4; j++) bits[j] = bits_raw<T>(mask, tile, j, lane);
         }
     }
+    __device__ __forceinline__ uint32_t valid(int j, int lane) const { return MASK ? bits_fix<T>(bits[j], lane) : 0u; }
 };
 template <typename T, bool PAD> __device__ __forceinline__ void unpack_group(const u32x4 &r, int left, float (&x)[Elem<T>::EPL]) {
-    Elem<T>::unpack(r, x);
+    unpack_fresh<T>(r, x);
     if (PAD) {
 #pragma unroll
         for (int k = 0; k < Elem<T>::EPL; k++) x[k] = k < left ? x[k] : -INFINITY;
     }
 }
-
-// One tile's tokens into the sums over all tokens and, with a mask, over the valid ones.  ALL: the former are wanted.
-template <typename T, bool MASK, bool ALL, bool W, bool PAD>
-__device__ __forceinline__ void take_tile(const MaskedTile<T> &mt, int left, int lane, float c, Sums &all, Sums &valid) {
-    constexpr int EPL = Elem<T>::EPL;
+template <typename T, bool MASK, bool W, bool PAD>
+__device__ __forceinline__ void take_tile_as(const MaskedTile<T, MASK> &mt, int left, int lane, float c, float step, Tally &a) {
 #pragma unroll
     for (int j = 0; j < 4; j++) {
-        float x[EPL];
+        float x[Elem<T>::EPL];
         unpack_group<T, PAD>(mt.t.r[j], left - j * TileGeom<T>::PER_LOAD, x);
-        if (ALL) take<EPL, W && !MASK>(all, x, c);
-        if (MASK) {
-            const uint32_t bits = bits_fix<T>(mt.bits[j], lane);
-            if (__ballot(bits != 0u) != 0ull) {
-#pragma unroll
-                for (int k = 0; k < EPL; k++) x[k] = if_bit(x[k], bits, k);
-                take<EPL, W>(valid, x, c);
-            }
-        }
+        const uint32_t bits = mt.valid(j, lane);
+        if (MASK) a.seen |= bits;
+        take_group<Elem<T>::EPL, MASK, W>(a, x, bits, c, step);
+        __builtin_amdgcn_sched_barrier(0);   // one group's tokens in registers at a time
     }
 }
-// The tiles first, first + step, ... of a row
-template <typename T, bool MASK, bool ALL, bool W>
-__device__ __forceinline__ void take_row(const Row &row, const Row &mask, int V, int first, int step, int lane, float c, Sums &all, Sums &valid) {
-    const int nt = (V + TileGeom<T>::TILE - 1) / TileGeom<T>::TILE;
-    MaskedTile<T> now, next;
-    now.template load<MASK>(row, mask, first, lane);
-    for (int t = first; t < nt; t += step) {
-        next.template load<MASK>(row, mask, t + step, lane);   // (behind the row: nothing is read)
-        const int left = tokens_left<T>(V, t, lane);
-        if ((t + 1) * TileGeom<T>::TILE <= V) take_tile<T, MASK, ALL, W, false>(now, left, lane, c, all, valid);
-        else take_tile<T, MASK, ALL, W, true>(now, left, lane, c, all, valid);
+template <typename T, bool MASK, bool W>
+__device__ __forceinline__ void take_tile(const MaskedTile<T, MASK> &mt, int tile, int V, int lane, float c, float step, Tally &a) {
+    const int left = tokens_left<T>(V, tile, lane);
+    if ((tile + 1) * TileGeom<T>::TILE <= V) take_tile_as<T, MASK, W, false>(mt, left, lane, c, step, a);
+    else take_tile_as<T, MASK, W, true>(mt, left, lane, c, step, a);
+}
+// The wavefront's tiles from its i-th on: the next one is on its way while one is summed.
+template <typename T, bool MASK, bool W>
+__device__ __forceinline__ void take_tiles(const Row &row, const Row &mask, int V, const Share &share, int i, int lane, float c, float step, Tally &a) {
+    if (i >= share.n) return;
+    MaskedTile<T, MASK> now, next;
+    now.load(row, mask, share.at(i), lane);
+    for (; i < share.n; i++) {
+        next.load(row, mask, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane);
+        take_tile<T, MASK, W>(now, share.at(i), V, lane, c, step, a);
         now = next;
     }
 }
 
-// Sums of a workgroup's wavefronts, to every wavefront.
-struct RowSums {
-    Sums all[MOST_WAVES], valid[MOST_WAVES];
+// The careful form, token by token relative to the largest one so far.
+template <int N> __device__ __forceinline__ void take_careful(Sums &a, const float (&x)[N], float c) {
+    const float m = most(most_of<N>(x, a.m), LOWEST);
+    refer(a.s, a.w, most((a.m - m) * c, FAINT));
+    a.m = m;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const float y = (x[i] - m) * c, e = fast_exp2(y);
+        a.s += e;
+        a.w = fmaf(most(y, FAINT), e, a.w);
+    }
+}
+__device__ __forceinline__ Sums over_lanes(Sums a, float c) {
+    const float m = wave_max(a.m);
+    refer(a.s, a.w, most((a.m - m) * c, FAINT));
+    return {m, wave_sum(a.s), wave_sum(a.w)};
+}
+template <typename T, bool MASK>
+__device__ __forceinline__ void take_row_careful(const Row &row, const Row &mask, int V, int wave, int nw, int lane, float c, Sums &all, Sums &valid) {
+    constexpr int EPL = Elem<T>::EPL;
+    all = valid = no_sums();
+#pragma unroll 1
+    for (int v = (wave * WAVE + lane) * EPL; v < V; v += nw * WAVE * EPL) {   // (as little code as it takes)
+        float x[EPL];
+        unpack_group<T, true>(__builtin_amdgcn_raw_buffer_load_b128(row.buf, (uint32_t)v * (uint32_t)sizeof(T), 0, 0), V - v, x);
+        take_careful<EPL>(all, x, c);
+        if (MASK) {
+            const uint32_t bits = bits_fix<T>(__builtin_amdgcn_raw_buffer_load_b8(mask.buf, (uint32_t)v >> 3, 0, 0), lane);
+#pragma unroll
+            for (int k = 0; k < EPL; k++) x[k] = if_bit(x[k], bits, k);
+            take_careful<EPL>(valid, x, c);
+        }
+    }
+    all = over_lanes(all, c);
+    valid = over_lanes(valid, c);
+}
+
+// What the wavefronts of a workgroup have found, to every one of them.
+struct RowShared {
+    Run all[MOST_WAVES], valid[MOST_WAVES];
+    Sums careful_all[MOST_WAVES], careful_valid[MOST_WAVES];
+    float top[MOST_WAVES];
+    uint32_t seen[MOST_WAVES];
     float x;   // the row's token's logit
 };
-template <bool W> __device__ __forceinline__ Sums over_waves(const Sums *part, int nw, int lane, float c) {
-    return over_wave<W>(lane < nw ? part[lane] : no_sums(), c);
+struct RowSums {
+    Sums all, q;   // over all tokens, and over the valid ones
+    float x;       // the row's token's logit
+};
+// `x`: known to wavefront 0.  By every wavefront of the row (ONE: the only one).  ONLY: the tally is of the valid tokens alone, and so is the
+// result.
+template <typename T, bool MASK, bool W, bool ONE, bool ONLY = false>
+__device__ __forceinline__ RowSums row_sums(RowShared &sh, const Row &row, const Row &mask, int V, const Tally &a, float x, int wave, int nw, int lane, float c) {
+    constexpr bool TWO = MASK && !ONLY;   // two sets of sums
+    Run all = over_lanes<W && !TWO>(a.all), valid = no_run();
+    float top = wave_max(a.top);
+    bool seen = false;
+    if (TWO) {
+        valid = over_lanes<W>(both<W>({a.all.r, a.s, a.w}, a.few));
+        seen = __ballot(a.seen != 0u) != 0ull;
+    }
+    if (!ONE) {
+        if (lane == 0) {
+            sh.all[wave] = all;
+            sh.top[wave] = top;
+            if (TWO) {
+                sh.valid[wave] = valid;
+                sh.seen[wave] = seen ? 1u : 0u;
+            }
+            if (wave == 0) sh.x = x;   // (read before a wavefront may write there)
+        }
+        __syncthreads();
+        const int i = lane < nw ? lane : 0;
+        all = over_lanes<W && !TWO>(lane < nw ? sh.all[i] : no_run());
+        top = wave_max(sh.top[i]);
+        if (TWO) {
+            valid = over_lanes<W>(lane < nw ? sh.valid[i] : no_run());
+            seen = __ballot(sh.seen[i] != 0u) != 0ull;
+        }
+        x = sh.x;
+    }
+    const bool far = fabsf(top) < INFINITY && (fabsf(top * c) >= FAR_OFF || (TWO && seen && valid.s == 0.f));
+    RowSums r;
+    r.x = x;
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(far), 0)) {   // (the same for all wavefronts of the row)
+        take_row_careful<T, MASK>(row, mask, V, wave, nw, lane, c, r.all, r.q);
+        if (!ONE) {
+            if (lane == 0) {
+                sh.careful_all[wave] = r.all;
+                sh.careful_valid[wave] = r.q;
+            }
+            __syncthreads();
+            r.all = over_lanes(lane < nw ? sh.careful_all[lane] : no_sums(), c);
+            r.q = over_lanes(lane < nw ? sh.careful_valid[lane] : no_sums(), c);
+        }
+        if (!MASK) r.q = r.all;
+        return r;
+    }
+    r.all = sums_of(all, c);
+    r.q = TWO ? sums_of(valid, c) : r.all;
+    return r;
 }
 
 // The row's token's logit; -inf where there is no such token, or it is not valid.
@@ -175,13 +361,14 @@ template <typename T, bool MASK, bool W, bool ONE>
 __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void score_kernel(const T *__restrict__ logits, int64_t row_stride,
                                                                                          const int32_t *__restrict__ tokens, const uint32_t *__restrict__ mask,
                                                                                          int V, int n_words, int B, Outputs out, Temper tp) {
-    __shared__ RowSums sh;
+    __shared__ RowShared sh;
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = ONE ? 1 : blockDim.x / WAVE;
-    const int per = ONE ? SHORT_ROWS : 1;
+    const int per = ONE ? SHORT_ROWS : 1, first = ONE ? 0 : wave;
+    const float step = RAISE * __builtin_amdgcn_rcpf(tp.c);
     for (int64_t b = (int64_t)blockIdx.x * per + (ONE ? wave : 0); b < B; b += (int64_t)gridDim.x * per) {
-        const int tok = tokens ? tokens[b] : 0;
+        const int tok = tokens ? tokens[b] : V;
         if (tok < 0) {   // left out
-            if (ONE ? lane == 0 : threadIdx.x == 0) {
+            if (lane == 0 && first == 0) {
                 put_values(out, b, {0.f, 0.f, 0.f});
                 if (out.stats) put_stats(out.stats, b, {0.f, 0.f, 0.f}, {0.f, 0.f, 0.f}, {0.f, 0.f, 0.f});
             }
@@ -189,27 +376,14 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
         }
         const T *at = logits + b * row_stride;
         const Row row = row_of(at, V), mrow = MASK ? mask_of(mask, b, n_words) : row;
-        const float x = tokens ? logit_of(at, MASK ? mask + b * n_words : nullptr, tok, V) : -INFINITY;
-        Sums all = no_sums(), valid = no_sums();
-        take_row<T, MASK, true, W>(row, mrow, V, ONE ? 0 : wave, nw, lane, tp.c, all, valid);
-        all = over_wave<W && !MASK>(all, tp.c);
-        if (MASK) valid = over_wave<W>(valid, tp.c);
-        if (!ONE) {
-            if (lane == 0) {
-                sh.all[wave] = all;
-                if (MASK) sh.valid[wave] = valid;
-            }
-            __syncthreads();
-            if (wave == 0) {
-                all = over_waves<W && !MASK>(sh.all, nw, lane, tp.c);
-                if (MASK) valid = over_waves<W>(sh.valid, nw, lane, tp.c);
-            }
-        }
-        if (lane == 0 && (ONE || wave == 0)) {
-            const Sums q = MASK ? valid : all;
-            const RowValues v = row_values<MASK>(all, q, x, tp);
+        const float x = first == 0 ? logit_of(at, MASK ? mask + b * n_words : nullptr, tok, V) : 0.f;
+        Tally a = no_tally();
+        take_tiles<T, MASK, W>(row, mrow, V, share_of(tiles_in<T>(V), first, nw), 0, lane, tp.c, step, a);
+        const RowSums r = row_sums<T, MASK, W, ONE>(sh, row, mrow, V, a, x, first, nw, lane, tp.c);
+        if (lane == 0 && first == 0) {
+            const RowValues v = row_values<MASK>(r.all, r.q, r.x, tp);
             put_values(out, b, v);
-            if (out.stats) put_stats(out.stats, b, all, q, v);
+            if (out.stats) put_stats(out.stats, b, r.all, r.q, v);
         }
         if (!ONE) __syncthreads();   // before LDS is used again
     }
@@ -220,23 +394,35 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
 struct Upstream {
     const float *logprobs, *logZ_valid, *entropy;
 };
-// d_logits = e_q (a + b y_q) - z e_p, and `at_token` more at the row's token; e_q = 2^y_q, y_q = (x - mq) c, e_p = 2^((x - mp) c).
+// d_logits = e_q (a + b y_q) - z e_p, and `at_token` more at the row's token.  y_q = x c - rq, e_q = 2^y_q, e_p = 2^(x c - rp); in rows
+// beyond FAR_OFF y_q = (x - rq) c and e_p likewise.
 struct Slope {
-    float mq, a, b, mp, z, at_token;
+    float rq, a, b, rp, z, at_token;
     bool nothing;   // zeros all over the row
+    bool far;
 };
 template <bool MASK> __device__ __forceinline__ Slope slope_of(const Sums &all, const Sums &q, float entropy, float logprob, const Upstream &up, int64_t b, int tok, const Temper &tp) {
     Slope s;
     const float g = up.logprobs && logprob > -INFINITY ? up.logprobs[b] : 0.f;   // (a log probability of -inf has no slope)
     const float z = MASK && up.logZ_valid ? up.logZ_valid[b] : 0.f, h = up.entropy ? up.entropy[b] : 0.f;
-    s.nothing = tok < 0 || !(q.s != 0.f);
-    const float over = tp.inv / q.s;
-    s.mq = q.m;
+    const float over = tp.inv / q.s, c = tp.c;
+    s.nothing = __builtin_amdgcn_readfirstlane(tok < 0 || !(q.s != 0.f));
+    s.far = __builtin_amdgcn_readfirstlane(!(fabsf(q.m * c) < FAR_OFF && fabsf(all.m * c) < FAR_OFF));
     s.a = over * (z - g - h * (entropy - logf(q.s)));
     s.b = over * (-LN2F * h);
-    s.mp = all.m;
-    s.z = MASK ? z * tp.inv / all.s : 0.f;
+    s.z = MASK && z != 0.f ? z * tp.inv / all.s : 0.f;
+    s.rq = q.m;
+    s.rp = all.m;
+    if (!s.far) {   // relative to m c as it is rounded
+        s.rq = q.m * c;
+        s.rp = all.m * c;
+        const float dq = fmaf(-q.m, c, s.rq), fq = fast_exp2(dq);
+        s.a = fq * fmaf(s.b, dq, s.a);
+        s.b *= fq;
+        s.z *= fast_exp2(fmaf(-all.m, c, s.rp));
+    }
     s.at_token = g * tp.inv;
+    s.rq = uniform(s.rq), s.a = uniform(s.a), s.b = uniform(s.b), s.rp = uniform(s.rp), s.z = uniform(s.z), s.at_token = uniform(s.at_token);
     return s;
 }
 // Values of this lane's tokens from token v on, rounded to the nearest of their type, once.  What lies behind the row is left as it is.
@@ -263,28 +449,44 @@ __device__ __forceinline__ void put_group(uint16_t *row, int v, int V, const flo
     for (int k = 0; k < 8; k++)
         if (v + k < V) row[v + k] = (uint16_t)(r[k / 2] >> (16 * (k & 1)));
 }
-template <typename T, bool MASK, bool H>
-__device__ __forceinline__ void put_tile(T *out, const MaskedTile<T> &mt, const Slope &s, int tile, int lane, int tok, int V, float c) {
+template <bool FAR> __device__ __forceinline__ float exponent(float x, float r, float c) { return FAR ? (x - r) * c : fmaf(x, c, -r); }
+template <typename T, bool MASK, bool H, bool FAR>
+__device__ __forceinline__ void put_tile_as(T *out, const MaskedTile<T, MASK> &mt, const Slope &s, int tile, int lane, int tok, int V, float c) {
     using G = TileGeom<T>;
 #pragma unroll
     for (int j = 0; j < 4; j++) {
         const int v = tile * G::TILE + j * G::PER_LOAD + lane * G::EPL;
         float x[G::EPL], d[G::EPL];
-        Elem<T>::unpack(mt.t.r[j], x);
-        const uint32_t bits = MASK ? bits_fix<T>(mt.bits[j], lane) : 0u;
-        const int mine = tok - v;   // the row's token, counted from this lane's first one
+        unpack_fresh<T>(mt.t.r[j], x);
+        const uint32_t bits = mt.valid(j, lane);
+        if (!MASK || __ballot(bits != 0u) != 0ull) {
 #pragma unroll
-        for (int k = 0; k < G::EPL; k++) {
-            const float y = (x[k] - s.mq) * c, e = fast_exp2(y);
-            float g = e * (H ? fmaf(s.b, most(y, FAINT), s.a) : s.a);
-            if (MASK) {
-                g = (bits >> k) & 1u ? g : 0.f;
-                g = fmaf(-s.z, fast_exp2((x[k] - s.mp) * c), g);
+            for (int k = 0; k < G::EPL; k++) {
+                const float y = exponent<FAR>(x[k], s.rq, c), e = fast_exp2(y);
+                d[k] = e * (H ? fmaf(s.b, most(y, FAINT), s.a) : s.a);
+                if (MASK) d[k] = (bits >> k) & 1u ? d[k] : 0.f;
             }
-            d[k] = mine == k ? g + s.at_token : g;
+        } else {
+#pragma unroll
+            for (int k = 0; k < G::EPL; k++) d[k] = 0.f;
+        }
+        if (MASK && s.z != 0.f) {
+#pragma unroll
+            for (int k = 0; k < G::EPL; k++) d[k] = fmaf(-s.z, fast_exp2(exponent<FAR>(x[k], s.rp, c)), d[k]);
+        }
+        const int mine = tok - v;   // the row's token, counted from this lane's first one
+        if (__ballot((uint32_t)mine < (uint32_t)G::EPL) != 0ull) {
+#pragma unroll
+            for (int k = 0; k < G::EPL; k++) d[k] = mine == k ? d[k] + s.at_token : d[k];
         }
         put_group(out, v, V, d);
+        __builtin_amdgcn_sched_barrier(0);   // one group's tokens in registers at a time
     }
+}
+template <typename T, bool MASK, bool H>
+__device__ __forceinline__ void put_tile(T *out, const MaskedTile<T, MASK> &mt, const Slope &s, int tile, int lane, int tok, int V, float c) {
+    if (__builtin_expect(s.far, 0)) put_tile_as<T, MASK, H, true>(out, mt, s, tile, lane, tok, V, c);
+    else put_tile_as<T, MASK, H, false>(out, mt, s, tile, lane, tok, V, c);
 }
 template <typename T> __device__ __forceinline__ void put_zeros(T *out, int first, int step, int lane, int V) {
     using G = TileGeom<T>;
@@ -293,17 +495,15 @@ template <typename T> __device__ __forceinline__ void put_zeros(T *out, int firs
 #pragma unroll
         for (int j = 0; j < 4; j++) put_group(out, t * G::TILE + j * G::PER_LOAD + lane * G::EPL, V, d);
 }
+// The wavefront's tiles from its i-th on; each is read before another one is written: out may be the logits themselves.
 template <typename T, bool MASK, bool H>
-__device__ __forceinline__ void put_row(T *out, const Row &row, const Row &mask, const Slope &s, int tok, int V, int first, int step, int lane, float c) {
-    if (s.nothing) {
-        put_zeros<T>(out, first, step, lane, V);
-        return;
-    }
-    MaskedTile<T> now, next;
-    now.template load<MASK>(row, mask, first, lane);
-    for (int t = first; t * TileGeom<T>::TILE < V; t += step) {
-        next.template load<MASK>(row, mask, t + step, lane);   // (read before this tile is written: out may be the logits themselves)
-        put_tile<T, MASK, H>(out, now, s, t, lane, tok, V, c);
+__device__ __forceinline__ void put_tiles(T *out, const Row &row, const Row &mask, const Slope &s, int tok, int V, const Share &share, int i, int lane, float c) {
+    if (i >= share.n) return;
+    MaskedTile<T, MASK> now, next;
+    now.load(row, mask, share.at(i), lane);
+    for (; i < share.n; i++) {
+        next.load(row, mask, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane);
+        put_tile<T, MASK, H>(out, now, s, share.at(i), lane, tok, V, c);
         now = next;
     }
 }
@@ -323,51 +523,58 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void gra
         const float *st = stats + b * PPV_LOGPROB_STATS;
         const Sums all = {st[0], st[1], 0.f}, q = {st[2], st[3], 0.f};
         const Slope s = slope_of<MASK>(all, q, st[4], st[5], up, b, tok, tp);
+        T *to = d_logits + b * d_row_stride;
+        const int first = ONE ? 0 : part * nw + wave, of = ONE ? 1 : nw * parts;
+        if (s.nothing) {
+            put_zeros(to, first, of, lane, V);
+            continue;
+        }
         const Row row = row_of(logits + b * row_stride, V);
-        put_row<T, MASK, H>(d_logits + b * d_row_stride, row, MASK ? mask_of(mask, b, n_words) : row, s, tok, V, ONE ? 0 : part * nw + wave,
-                            ONE ? 1 : nw * parts, lane, tp.c);
+        put_tiles<T, MASK, H>(to, row, MASK ? mask_of(mask, b, n_words) : row, s, tok, V, share_of(tiles_in<T>(V), first, of), 0, lane, tp.c);
     }
 }
 
-// Both: the sums, then the gradient from the row read again (from cache).
-template <typename T, bool MASK, bool W, bool ONE>
+// Both: the sums, then the gradient.  A wavefront holds its first HELD tiles; what is more is read again, from cache.
+template <typename T, bool MASK, bool W, bool ONE, int HELD>
 __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void score_gradient_kernel(const T *logits, int64_t row_stride, const int32_t *__restrict__ tokens,
                                                                                                   const uint32_t *__restrict__ mask, int V, int n_words, int B,
                                                                                                   T *d_logits, int64_t d_row_stride, Outputs out, Upstream up, Temper tp) {
-    __shared__ RowSums sh;
+    __shared__ RowShared sh;
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = ONE ? 1 : blockDim.x / WAVE;
     const int per = ONE ? SHORT_ROWS : 1, first = ONE ? 0 : wave;
+    const float step = RAISE * __builtin_amdgcn_rcpf(tp.c);
     for (int64_t b = (int64_t)blockIdx.x * per + (ONE ? wave : 0); b < B; b += (int64_t)gridDim.x * per) {
         const int tok = tokens ? tokens[b] : V;
         T *to = d_logits + b * d_row_stride;
         if (tok < 0) {   // left out
             if (lane == 0 && first == 0) put_values(out, b, {0.f, 0.f, 0.f});
-            put_zeros<T>(to, first, nw, lane, V);
+            put_zeros(to, first, nw, lane, V);
             continue;
         }
         const T *at = logits + b * row_stride;
         const Row row = row_of(at, V), mrow = MASK ? mask_of(mask, b, n_words) : row;
-        float x = first == 0 ? logit_of(at, MASK ? mask + b * n_words : nullptr, tok, V) : 0.f;
-        Sums all = no_sums(), valid = no_sums();
-        take_row<T, MASK, true, W>(row, mrow, V, first, nw, lane, tp.c, all, valid);
-        all = over_wave<W && !MASK>(all, tp.c);
-        if (MASK) valid = over_wave<W>(valid, tp.c);
-        if (!ONE) {
-            if (lane == 0) {
-                sh.all[wave] = all;
-                if (MASK) sh.valid[wave] = valid;
-                if (wave == 0) sh.x = x;   // (read before a wavefront may write there)
-            }
-            __syncthreads();
-            x = sh.x;
-            all = over_waves<W && !MASK>(sh.all, nw, lane, tp.c);
-            if (MASK) valid = over_waves<W>(sh.valid, nw, lane, tp.c);
-        }
-        const Sums q = MASK ? valid : all;
-        const RowValues v = row_values<MASK>(all, q, x, tp);
+        const Share share = share_of(tiles_in<T>(V), first, nw);
+        MaskedTile<T, MASK> held[HELD];
+#pragma unroll
+        for (int i = 0; i < HELD; i++) held[i].load(row, mrow, i < share.n ? share.at(i) : NO_TILE, lane);
+        const float x = first == 0 ? logit_of(at, MASK ? mask + b * n_words : nullptr, tok, V) : 0.f;
+        Tally a = no_tally();
+#pragma unroll
+        for (int i = 0; i < HELD; i++)
+            if (i < share.n) take_tile<T, MASK, W>(held[i], share.at(i), V, lane, tp.c, step, a);
+        take_tiles<T, MASK, W>(row, mrow, V, share, HELD, lane, tp.c, step, a);
+        const RowSums r = row_sums<T, MASK, W, ONE>(sh, row, mrow, V, a, x, first, nw, lane, tp.c);
+        const RowValues v = row_values<MASK>(r.all, r.q, r.x, tp);
         if (lane == 0 && first == 0) put_values(out, b, v);
-        const Slope s = slope_of<MASK>(all, q, v.entropy, v.logprob, up, b, tok, tp);
-        put_row<T, MASK, W>(to, row, mrow, s, tok, V, first, nw, lane, tp.c);
+        const Slope s = slope_of<MASK>(r.all, r.q, v.entropy, v.logprob, up, b, tok, tp);
+        if (s.nothing) {
+            put_zeros(to, first, nw, lane, V);
+        } else {
+#pragma unroll
+            for (int i = 0; i < HELD; i++)
+                if (i < share.n) put_tile<T, MASK, W>(to, held[i], s, share.at(i), lane, tok, V, tp.c);
+            put_tiles<T, MASK, W>(to, row, mrow, s, tok, V, share, HELD, lane, tp.c);
+        }
         if (!ONE) __syncthreads();   // before LDS is used again
     }
 }
@@ -389,12 +596,16 @@ __device__ __forceinline__ uint64_t key_of(float x, int v) {
     return x == -INFINITY ? 0ull : (uint64_t)order_of(x) << TOKEN_BITS | (TOKEN_MASK - (uint32_t)v);
 }
 
+constexpr int MOST_LISTED = 1024;   // candidates not below the bound that are sorted out in LDS
 struct TopShared {
-    RowSums sums;
-    uint32_t bin[BINS];
-    uint64_t list[PPV_TOP_MAX];
+    RowShared row;
+    union {
+        uint32_t best[MOST_WAVES * WAVE];   // each lane's largest token, and (up to eight wavefronts) the largest of its other groups
+        uint32_t bin[BINS];
+    };
+    uint64_t list[MOST_LISTED];
     uint64_t prefix;
-    uint32_t n, want;
+    uint32_t n, want, bound;
     int settled;
 };
 // every candidate of the row, one lane and one token at a time: f(key)
@@ -402,14 +613,14 @@ template <typename T, bool MASK, typename F>
 __device__ __forceinline__ void each_candidate(const Row &row, const Row &mask, int V, int first, int step, int lane, F f) {
     using G = TileGeom<T>;
     for (int t = first; t * G::TILE < V; t += step) {
-        MaskedTile<T> mt;
-        mt.template load<MASK>(row, mask, t, lane);
+        MaskedTile<T, MASK> mt;
+        mt.load(row, mask, t, lane);
 #pragma unroll
         for (int j = 0; j < 4; j++) {
             float x[G::EPL];
             const int v = t * G::TILE + j * G::PER_LOAD + lane * G::EPL;
             unpack_group<T, true>(mt.t.r[j], V - v, x);
-            const uint32_t bits = MASK ? bits_fix<T>(mt.bits[j], lane) : 0xFFu;
+            const uint32_t bits = MASK ? mt.valid(j, lane) : 0xFFu;
 #pragma unroll
             for (int k = 0; k < G::EPL; k++) {
                 const uint64_t key = (bits >> k) & 1u ? key_of(x[k], v + k) : 0ull;
@@ -466,18 +677,80 @@ __device__ __forceinline__ void select_row(TopShared &sh, const Row &row, const 
     each_candidate<T, MASK>(row, mask, V, wave, nw, lane, [&](uint64_t key) __attribute__((always_inline)) {
         if (key >= least) {
             const uint32_t i = atomicAdd(&sh.n, 1u);
-            if (i < PPV_TOP_MAX) sh.list[i] = key;   // (at most k of them)
+            if (i < MOST_LISTED) sh.list[i] = key;   // (k of them, or all there are)
         }
     });
     __syncthreads();
 }
 
+// What a lane remembers of its groups of tokens (16 bytes each) beside their sums: the group with the largest token, and the largest token
+// of the others.
+struct Best {
+    float first, second;
+    int at;   // 4 i + j: load j of the wavefront's i-th tile
+};
+template <typename T, bool MASK, bool W, bool PAD>
+__device__ __forceinline__ void top_tile_as(const MaskedTile<T, MASK> &mt, int i, int left, int lane, float c, float step, Tally &a, Best &best) {
+    constexpr int EPL = Elem<T>::EPL;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        const uint32_t bits = mt.valid(j, lane);
+        if (MASK && __ballot(bits != 0u) == 0ull) continue;
+        float x[EPL];
+        unpack_group<T, PAD>(mt.t.r[j], left - j * TileGeom<T>::PER_LOAD, x);
+        if (MASK) {
+#pragma unroll
+            for (int k = 0; k < EPL; k++) x[k] = if_bit(x[k], bits, k);
+        }
+        const float g = most_of<EPL>(x, -INFINITY);
+        a.top = most(a.top, g);
+        raise<false>(a, c, step);
+        add<EPL, W>(a.all, x, c);
+        best.second = __builtin_amdgcn_fmed3f(best.first, best.second, g);   // (second <= first)
+        best.at = g > best.first ? 4 * i + j : best.at;
+        best.first = most(best.first, g);
+        __builtin_amdgcn_sched_barrier(0);   // one group's tokens in registers at a time
+    }
+}
+// The k-th largest of the lanes' largest tokens, or a little less: at least k tokens are not below it.  1 where fewer lanes have any.  By
+// one wavefront, bit by bit from the top.  Up to QUARTER candidates the lanes' tokens are taken four at a time, which costs a bound that a few
+// more tokens reach and a quarter of the comparisons.
+constexpr int QUARTER = 64, BOUND_BITS = 16;
+template <int N> __device__ __forceinline__ uint32_t bound_of(const uint32_t (&u)[N], int k) {
+    uint32_t t = 0u;
+#pragma unroll 1
+    for (int bit = 31; bit >= 32 - BOUND_BITS; bit--) {
+        const uint32_t try_at = t | 1u << bit;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; i++) n += __popcll(__ballot(u[i] >= try_at));
+        if (n >= k) t = try_at;
+        if (n == k) break;
+    }
+    return t > 1u ? t : 1u;
+}
+template <typename T>
+__device__ __forceinline__ void list_group(TopShared &sh, const u32x4 &raw, uint32_t bits, int v, int V, uint32_t bound) {
+    constexpr int EPL = Elem<T>::EPL;
+    float x[EPL];
+    unpack_group<T, true>(raw, V - v, x);
+#pragma unroll
+    for (int k = 0; k < EPL; k++) {
+        const uint64_t key = (bits >> k) & 1u ? key_of(x[k], v + k) : 0ull;
+        if (key >> TOKEN_BITS >= bound) {
+            const uint32_t i = atomicAdd(&sh.n, 1u);
+            if (i < MOST_LISTED) sh.list[i] = key;
+        }
+    }
+}
 template <typename T, bool MASK, bool W>
 __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restrict__ logits, int64_t row_stride, const int32_t *__restrict__ tokens,
                                                               const uint32_t *__restrict__ mask, int V, int n_words, int B, int k,
                                                               int32_t *__restrict__ top_ids, float *__restrict__ top_logprobs, Outputs out, Temper tp) {
+    using G = TileGeom<T>;
     __shared__ TopShared sh;
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = blockDim.x / WAVE;
+    const float step = RAISE * __builtin_amdgcn_rcpf(tp.c);
     for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
         const int tok = tokens ? tokens[b] : V;
         int32_t *ids = top_ids + b * k;
@@ -492,29 +765,81 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
         }
         const T *at = logits + b * row_stride;
         const Row row = row_of(at, V), mrow = MASK ? mask_of(mask, b, n_words) : row;
-        const float x = logit_of(at, MASK ? mask + b * n_words : nullptr, tok, V);
-        Sums q = no_sums(), valid = no_sums();
-        take_row<T, MASK, !MASK, W>(row, mrow, V, wave, nw, lane, tp.c, q, valid);
-        if (MASK) q = valid;
-        q = over_wave<W>(q, tp.c);
-        if (lane == 0) sh.sums.all[wave] = q;
+        const float x = wave == 0 ? logit_of(at, MASK ? mask + b * n_words : nullptr, tok, V) : 0.f;
+        const Share share = share_of(tiles_in<T>(V), wave, nw);
+        Tally a = no_tally();
+        Best best = {-INFINITY, -INFINITY, 0};
+        {
+            MaskedTile<T, MASK> now, next;
+            now.load(row, mrow, share.n ? share.at(0) : NO_TILE, lane);
+            for (int i = 0; i < share.n; i++) {
+                next.load(row, mrow, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane);
+                const int tile = share.at(i), left = tokens_left<T>(V, tile, lane);
+                if ((tile + 1) * G::TILE <= V) top_tile_as<T, MASK, W, false>(now, i, left, lane, tp.c, step, a, best);
+                else top_tile_as<T, MASK, W, true>(now, i, left, lane, tp.c, step, a, best);
+                now = next;
+            }
+        }
+        const uint32_t mine = best.first == -INFINITY ? 0u : order_of(best.first);
+        const uint32_t other = best.second == -INFINITY ? 0u : order_of(best.second);
+        sh.best[wave * WAVE + lane] = mine;
+        if (nw * 2 <= MOST_WAVES) sh.best[(nw + wave) * WAVE + lane] = other;
+        if (threadIdx.x == 0) sh.n = 0;
+        const RowSums r = row_sums<T, MASK, W, false, true>(sh.row, row, mrow, V, a, x, wave, nw, lane, tp.c);   // (a barrier behind what is above)
+        if (threadIdx.x == 0) put_values(out, b, row_values<false>(r.q, r.q, r.x, tp));
+        if (wave == 0) {
+            uint32_t u[MOST_WAVES];
+#pragma unroll
+            for (int i = 0; i < MOST_WAVES; i++) u[i] = i < (nw * 2 <= MOST_WAVES ? 2 * nw : nw) ? sh.best[i * WAVE + lane] : 0u;
+            uint32_t bound;
+            if (k <= QUARTER) {
+                uint32_t q[MOST_WAVES / 4];
+#pragma unroll
+                for (int i = 0; i < MOST_WAVES / 4; i++) q[i] = max(max(u[i], u[i + 4]), max(u[i + 8], u[i + 12]));
+                bound = bound_of(q, k);
+            } else {
+                bound = bound_of(u, k);
+            }
+            if (lane == 0) sh.bound = bound;
+        }
         __syncthreads();
-        q = over_waves<W>(sh.sums.all, nw, lane, tp.c);
-        const RowValues v = row_values<false>(q, q, x, tp);
-        if (threadIdx.x == 0) put_values(out, b, v);
-        select_row<T, MASK>(sh, row, mrow, V, k, wave, nw, lane);
-        const int n = (int)min(sh.n, (uint32_t)k);
-        for (int i = threadIdx.x; i < k; i += blockDim.x) {   // a candidate's place: how many are larger
-            if (i >= n) {
+        const uint32_t bound = sh.bound;
+        const bool more = other >= bound;
+        auto look = [&](int i, int l) __attribute__((always_inline)) {   // at lane l's group i
+            const int v = share.at(i >> 2) * G::TILE + (i & 3) * G::PER_LOAD + l * G::EPL;
+            list_group<T>(sh, __builtin_amdgcn_raw_buffer_load_b128(row.buf, (uint32_t)v * (uint32_t)sizeof(T), 0, 0),
+                          MASK ? bits_fix<T>(__builtin_amdgcn_raw_buffer_load_b8(mrow.buf, (uint32_t)v >> 3, 0, 0), l) : 0xFFu, v, V, bound);
+        };
+        if (mine >= bound && !more) look(best.at, lane);
+        // lanes with more than one such group: all of theirs are looked at again, one lane's by the whole wavefront or each its own
+        const uint64_t lanes = __ballot(more);
+        if (__popcll(lanes) * ((share.n * 4 + WAVE - 1) / WAVE) > share.n * 4) {
+            if (more)
+                for (int i = 0; i < share.n * 4; i++) look(i, lane);
+        } else {
+            for (uint64_t rest = lanes; rest; rest &= rest - 1ull)
+                for (int i = lane; i < share.n * 4; i += WAVE) look(i, __ffsll((long long)rest) - 1);
+        }
+        __syncthreads();
+        uint32_t n = sh.n;
+        __syncthreads();
+        if (n > MOST_LISTED) {   // tokens that are too much alike
+            select_row<T, MASK>(sh, row, mrow, V, k, wave, nw, lane);
+            n = sh.n;
+        }
+        for (int i = threadIdx.x; i < k; i += blockDim.x)
+            if (i >= (int)n) {
                 ids[i] = -1;
                 lps[i] = -INFINITY;
-                continue;
             }
+        for (int i = threadIdx.x; i < (int)n; i += blockDim.x) {   // a candidate's place: how many are larger
             const uint64_t key = sh.list[i];
             int place = 0;
-            for (int j = 0; j < n; j++) place += sh.list[j] > key;
-            ids[place] = (int32_t)(TOKEN_MASK - ((uint32_t)key & TOKEN_MASK));
-            lps[place] = row_values<false>(q, q, logit_at((uint32_t)(key >> TOKEN_BITS)), tp).logprob;
+            for (int j = 0; j < (int)n; j++) place += sh.list[j] > key;
+            if (place < k) {
+                ids[place] = (int32_t)(TOKEN_MASK - ((uint32_t)key & TOKEN_MASK));
+                lps[place] = row_values<false>(r.q, r.q, logit_at((uint32_t)(key >> TOKEN_BITS)), tp).logprob;
+            }
         }
         __syncthreads();   // before LDS is used again
     }
@@ -653,10 +978,10 @@ extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, 
 #define PPV_SCORE_GRADIENT(T, MASK, ENTROPY)                                                                                            \
     do {                                                                                                                                \
         if (sh.one)                                                                                                                     \
-            hipLaunchKernelGGL((score_gradient_kernel<T, MASK, ENTROPY, true>), dim3(sh.grid), dim3(sh.block), 0, (hipStream_t)stream,  \
+            hipLaunchKernelGGL((score_gradient_kernel<T, MASK, ENTROPY, true, 1>), dim3(sh.grid), dim3(sh.block), 0, (hipStream_t)stream,  \
                                (const T *)logits, row_stride, tokens, mask, V, n_words, B, (T *)d_logits, d_row_stride, out, up, tp);   \
         else                                                                                                                            \
-            hipLaunchKernelGGL((score_gradient_kernel<T, MASK, ENTROPY, false>), dim3(sh.grid), dim3(sh.block), 0, (hipStream_t)stream, \
+            hipLaunchKernelGGL((score_gradient_kernel<T, MASK, ENTROPY, false, MASK ? 2 : 4>), dim3(sh.grid), dim3(sh.block), 0, (hipStream_t)stream, \
                                (const T *)logits, row_stride, tokens, mask, V, n_words, B, (T *)d_logits, d_row_stride, out, up, tp);   \
     } while (0)
     PPV_PICK(dt, mask, entropy || d_entropy, PPV_SCORE_GRADIENT);

@@ -197,6 +197,10 @@ def odd_values(kind, B, V, rng):
         x = np.tile(np.linspace(-20, 5, V), (B, 1))
     elif kind == "falling":
         x = np.tile(np.linspace(5, -20, V), (B, 1))
+    elif kind == "late peak":           # what is valid comes first and is far below what comes later; some of it far below the rest
+        x[:, V // 4:V // 2] -= 250.0
+        x[:, V // 2:] += 300.0
+        x[:, 3 * V // 4:] += 60.0
     elif kind == "low mass":            # the valid tokens far below the rest
         x[:, V // 2:] -= 300.0
     return x
@@ -204,7 +208,7 @@ def odd_values(kind, B, V, rng):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [100, 3001, 40000])
-@pytest.mark.parametrize("kind", ["filtered", "lowest", "high", "far", "ties", "peak", "rising", "falling", "low mass"])
+@pytest.mark.parametrize("kind", ["filtered", "lowest", "high", "far", "ties", "peak", "rising", "falling", "low mass", "late peak"])
 def test_odd_values(kind, V, dtype):
     rng = np.random.default_rng(V)
     B = 12
@@ -212,6 +216,8 @@ def test_odd_values(kind, V, dtype):
     valid = None if kind == "far" else hand_made_masks(B, V, rng)
     if kind == "low mass":
         valid[:, :V // 2] = False
+    if kind == "late peak":
+        valid[:, V // 2:] = False
     for v in (None, valid):
         tok = tokens_for(v, B, V, rng)
         c = Case(x, dtype, v, tok)
