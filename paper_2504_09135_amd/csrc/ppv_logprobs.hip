@@ -14,7 +14,6 @@ namespace {
 
 constexpr int MOST_WAVES = 16;       // wavefronts per row and workgroup
 constexpr int SHORT_ROWS = 4;        // rows of one tile: so many to a workgroup, a wavefront each
-constexpr unsigned MOST_GROUPS = 1u << 20;   // workgroups of a launch: more rows than that are taken in turns
 constexpr float LOWEST = -3.402823466e38f;
 constexpr float FAINT = -1000.f;     // as an exponent of 2: a weight of 0
 
@@ -49,7 +48,8 @@ __device__ __forceinline__ float uniform(float x) { return __int_as_float(__buil
 constexpr float FAR_OFF = 134217728.f;   // 2^27: below it the rounding of r is at most four units of the exponent
 constexpr float RAISE = 12.f;            // units of the exponent; entropies lose 12 * 2^-24 where a row's largest token comes late
 constexpr float FAINT_SUM = 9.09494702e-13f;   // 2^-40: valid tokens that weigh less than that against the lane's reference get one of their own
-constexpr float LOSES = -40.f;
+constexpr float LOSES = -60.f;           // raised by more than that at once, the valid tokens before may be lost: the careful form again
+constexpr uint32_t LOST = 1u << 31;
 struct Run {
     float r, s, w;
 };
@@ -66,7 +66,7 @@ struct Tally {
     float s, w;         // with a mask: the valid tokens relative to all.r ...
     Run few;            // ... and relative to a reference of their own
     float few_top, few_limit;
-    uint32_t seen;      // bits of the mask
+    uint32_t seen;      // bits of the mask; LOST
 };
 __device__ __forceinline__ Tally no_tally() { return {no_run(), -INFINITY, LOWEST, 0.f, 0.f, no_run(), -INFINITY, LOWEST, 0u}; }
 __device__ __forceinline__ void refer(float &s, float &w, float d) {   // to a reference that lies -d above
@@ -75,25 +75,17 @@ __device__ __forceinline__ void refer(float &s, float &w, float d) {   // to a r
     s *= f;
 }
 __device__ __forceinline__ float reference_at(float top, float c) { return most(top * c, -FAR_OFF); }
-template <bool W> __device__ __forceinline__ Run both(const Run &a, const Run &b) {
-    const float ra = a.s != 0.f ? a.r : LOWEST, rb = b.s != 0.f ? b.r : LOWEST, R = most(ra, rb);
-    const float da = most(ra - R, FAINT), db = most(rb - R, FAINT), fa = fast_exp2(da), fb = fast_exp2(db);
-    return {R, fa * a.s + fb * b.s, W ? fa * fmaf(da, a.s, a.w) + fb * fmaf(db, b.s, b.w) : 0.f};
-}
 // The lane's reference is raised to its largest token where that lies above the limit (lanes whose does not: nothing changes).
 template <bool MASK> __device__ __forceinline__ void raise(Tally &a, float c, float step) {
-    if (__ballot(a.top > a.limit) == 0ull) return;
-    const bool up = a.top > a.limit;
-    const float r = up ? reference_at(a.top, c) : a.all.r, d = a.all.r - r;
-    if (MASK && a.s != 0.f && d < LOSES) {   // the valid tokens so far would vanish against the new one
-        a.few = both<true>(a.few, {a.all.r, a.s, a.w});
-        a.few_limit = fmaf(a.few.r, __builtin_amdgcn_rcpf(c), step);
-        a.s = a.w = 0.f;
+    if (__ballot(a.top > a.limit) != 0ull) {
+        const bool up = a.top > a.limit;
+        const float r = up ? reference_at(a.top, c) : a.all.r, d = a.all.r - r;
+        if (MASK) a.seen |= a.s != 0.f && d < LOSES ? LOST : 0u;
+        refer(a.all.s, a.all.w, d);
+        if (MASK) refer(a.s, a.w, d);
+        a.all.r = r;
+        a.limit = up ? a.top + step : a.limit;
     }
-    refer(a.all.s, a.all.w, d);
-    if (MASK) refer(a.s, a.w, d);
-    a.all.r = r;
-    a.limit = up ? a.top + step : a.limit;
 }
 template <int N, bool W> __device__ __forceinline__ void add(Run &a, const float (&x)[N], float c) {
 #pragma unroll
@@ -114,11 +106,9 @@ template <int N, bool MASK, bool W> __device__ __forceinline__ void take_group(T
         add<N, W>(a.all, x, c);
         return;
     }
-    const uint64_t lanes = __ballot(bits != 0u);
     bool alone = bits != 0u;
-    if (__popcll(lanes) <= FEW_LANES) {
+    if (__popcll(__ballot(alone)) <= FEW_LANES) {
         add<N, false>(a.all, x, c);
-        if (lanes == 0ull) return;
     } else {
         float s = 0.f, w = 0.f;
 #pragma unroll
@@ -132,18 +122,21 @@ template <int N, bool MASK, bool W> __device__ __forceinline__ void take_group(T
         alone = alone && s < FAINT_SUM;
         a.s += alone ? 0.f : s;
         if (W) a.w += alone ? 0.f : w;
-        if (__ballot(alone) == 0ull) return;
     }
+    if (__ballot(alone) != 0ull) {
+        const uint32_t mine = alone ? bits : 0u;
 #pragma unroll
-    for (int i = 0; i < N; i++) x[i] = if_bit(x[i], alone ? bits : 0u, i);
-    a.few_top = most_of<N>(x, a.few_top);
-    if (a.few_top > a.few_limit) {
-        const float r = reference_at(a.few_top, c);
-        refer(a.few.s, a.few.w, a.few.r - r);
-        a.few.r = r;
-        a.few_limit = a.few_top + step;
+        for (int i = 0; i < N; i++) x[i] = if_bit(x[i], mine, i);
+        a.few_top = most_of<N>(x, a.few_top);
+        const bool up = a.few_top > a.few_limit;
+        if (__ballot(up) != 0ull) {
+            const float r = up ? reference_at(a.few_top, c) : a.few.r;
+            refer(a.few.s, a.few.w, a.few.r - r);
+            a.few.r = r;
+            a.few_limit = up ? a.few_top + step : a.few_limit;
+        }
+        add<N, W>(a.few, x, c);
     }
-    add<N, W>(a.few, x, c);
 }
 
 template <typename T> __device__ __forceinline__ int tiles_in(int V) { return (V + TileGeom<T>::TILE - 1) / TileGeom<T>::TILE; }
@@ -152,6 +145,11 @@ template <bool W> __device__ __forceinline__ Run over_lanes(const Run &a) {   //
     const float r = a.s != 0.f ? a.r : LOWEST, R = wave_max(r), d = most(r - R, FAINT), f = fast_exp2(d);
     return {R, wave_sum(f * a.s), W ? wave_sum(f * fmaf(d, a.s, a.w)) : 0.f};
 }
+template <bool W> __device__ __forceinline__ Run both(const Run &a, const Run &b) {
+    const float ra = a.s != 0.f ? a.r : LOWEST, rb = b.s != 0.f ? b.r : LOWEST, R = most(ra, rb);
+    const float da = most(ra - R, FAINT), db = most(rb - R, FAINT), fa = fast_exp2(da), fb = fast_exp2(db);
+    return {R, fa * a.s + fb * b.s, W ? fa * fmaf(da, a.s, a.w) + fb * fmaf(db, b.s, b.w) : 0.f};
+}
 // relative to a logit that makes the sum about 1: weights are then no smaller against it than they are
 __device__ __forceinline__ Sums sums_of(const Run &a, float c) {
     if (!(a.s != 0.f)) return no_sums();
@@ -159,33 +157,27 @@ __device__ __forceinline__ Sums sums_of(const Run &a, float c) {
     return {m, f * a.s, f * fmaf(d, a.s, a.w)};
 }
 
-// A row's mask as the memory unit's buffer; what is asked for behind its end is 0.
-__device__ __forceinline__ Row mask_of(const uint32_t *mask, int64_t b, int n_words) {
-    return row_of<uint32_t, 0u>(mask + b * n_words, n_words);
-}
-// Bits of this lane's tokens of load j of a tile: their byte (bf16), or half of it.
-template <typename T> __device__ __forceinline__ uint32_t bits_raw(const Row &mask, int tile, int j, int lane) {
-    const uint32_t v = (uint32_t)tile * TileGeom<T>::TILE + (uint32_t)j * TileGeom<T>::PER_LOAD + (uint32_t)lane * TileGeom<T>::EPL;
-    return __builtin_amdgcn_raw_buffer_load_b8(mask.buf, v >> 3, 0, 0);
-}
-template <typename T> __device__ __forceinline__ uint32_t bits_fix(uint32_t raw, int lane) {
-    return TileGeom<T>::EPL == 8 ? raw : (raw >> ((lane & 1) * 4)) & 0xFu;
-}
+// A tile of a row and, in each lane, a word of its mask.
 template <typename T, bool MASK> struct MaskedTile {
     RawTile t;
-    uint32_t bits[4];
-    __device__ __forceinline__ void load(const Row &row, const Row &mask, int tile, int lane) {
+    __device__ __forceinline__ void load(const Row &row, const uint32_t *mask, int tile, int lane, int V) {
         load_tile<T>(row, tile, lane, t);
-        if (MASK) {
-#pragma unroll
-            for (int j = 0; j < 4; j++) bits[j] = bits_raw<T>(mask, tile, j, lane);
-        }
+        if (MASK) t.word = tile_word_raw<T>(mask, tile, lane, V);
     }
-    __device__ __forceinline__ uint32_t valid(int j, int lane) const { return MASK ? bits_fix<T>(bits[j], lane) : 0u; }
+    // once it has come: bits behind the row's end are 0
+    __device__ __forceinline__ void settle(int tile, int lane, int V) {
+        if (MASK) t.word = tile_word_fix<T>(t.word, tile, lane, V);
+    }
+    __device__ __forceinline__ uint32_t valid(int j, int lane) const { return MASK ? lane_bits<T>(t.word, j, lane) : 0u; }
 };
+// Bits of the tokens of a group that starts with token v, read by themselves
+template <typename T> __device__ __forceinline__ uint32_t bits_at(const uint32_t *mask, int v, int V) {
+    return v < V ? (mask[v >> 5] >> (v & 31)) & ((1u << Elem<T>::EPL) - 1u) : 0u;
+}
 template <typename T, bool PAD> __device__ __forceinline__ void unpack_group(const u32x4 &r, int left, float (&x)[Elem<T>::EPL]) {
     unpack_fresh<T>(r, x);
     if (PAD) {
+        asm volatile("" : "+v"(left));   // (compared here: ahead of the loop over rows each token's comparison takes two scalar registers)
 #pragma unroll
         for (int k = 0; k < Elem<T>::EPL; k++) x[k] = k < left ? x[k] : -INFINITY;
     }
@@ -210,12 +202,13 @@ __device__ __forceinline__ void take_tile(const MaskedTile<T, MASK> &mt, int til
 }
 // The wavefront's tiles from its i-th on: the next one is on its way while one is summed.
 template <typename T, bool MASK, bool W>
-__device__ __forceinline__ void take_tiles(const Row &row, const Row &mask, int V, const Share &share, int i, int lane, float c, float step, Tally &a) {
+__device__ __forceinline__ void take_tiles(const Row &row, const uint32_t *mask, int V, const Share &share, int i, int lane, float c, float step, Tally &a) {
     if (i >= share.n) return;
     MaskedTile<T, MASK> now, next;
-    now.load(row, mask, share.at(i), lane);
+    now.load(row, mask, share.at(i), lane, V);
     for (; i < share.n; i++) {
-        next.load(row, mask, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane);
+        next.load(row, mask, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane, V);
+        now.settle(share.at(i), lane, V);
         take_tile<T, MASK, W>(now, share.at(i), V, lane, c, step, a);
         now = next;
     }
@@ -239,7 +232,7 @@ __device__ __forceinline__ Sums over_lanes(Sums a, float c) {
     return {m, wave_sum(a.s), wave_sum(a.w)};
 }
 template <typename T, bool MASK>
-__device__ __forceinline__ void take_row_careful(const Row &row, const Row &mask, int V, int wave, int nw, int lane, float c, Sums &all, Sums &valid) {
+__device__ __forceinline__ void take_row_careful(const Row &row, const uint32_t *mask, int V, int wave, int nw, int lane, float c, Sums &all, Sums &valid) {
     constexpr int EPL = Elem<T>::EPL;
     all = valid = no_sums();
 #pragma unroll 1
@@ -248,7 +241,7 @@ __device__ __forceinline__ void take_row_careful(const Row &row, const Row &mask
         unpack_group<T, true>(__builtin_amdgcn_raw_buffer_load_b128(row.buf, (uint32_t)v * (uint32_t)sizeof(T), 0, 0), V - v, x);
         take_careful<EPL>(all, x, c);
         if (MASK) {
-            const uint32_t bits = bits_fix<T>(__builtin_amdgcn_raw_buffer_load_b8(mask.buf, (uint32_t)v >> 3, 0, 0), lane);
+            const uint32_t bits = bits_at<T>(mask, v, V);
 #pragma unroll
             for (int k = 0; k < EPL; k++) x[k] = if_bit(x[k], bits, k);
             take_careful<EPL>(valid, x, c);
@@ -273,14 +266,14 @@ struct RowSums {
 // `x`: known to wavefront 0.  By every wavefront of the row (ONE: the only one).  ONLY: the tally is of the valid tokens alone, and so is the
 // result.
 template <typename T, bool MASK, bool W, bool ONE, bool ONLY = false>
-__device__ __forceinline__ RowSums row_sums(RowShared &sh, const Row &row, const Row &mask, int V, const Tally &a, float x, int wave, int nw, int lane, float c) {
+__device__ __forceinline__ RowSums row_sums(RowShared &sh, const Row &row, const uint32_t *mask, int V, const Tally &a, float x, int wave, int nw, int lane, float c) {
     constexpr bool TWO = MASK && !ONLY;   // two sets of sums
     Run all = over_lanes<W && !TWO>(a.all), valid = no_run();
     float top = wave_max(a.top);
-    bool seen = false;
+    uint32_t seen = 0u;
     if (TWO) {
         valid = over_lanes<W>(both<W>({a.all.r, a.s, a.w}, a.few));
-        seen = __ballot(a.seen != 0u) != 0ull;
+        seen = (__ballot(a.seen != 0u) ? 1u : 0u) | (__ballot(a.seen & LOST) ? LOST : 0u);
     }
     if (!ONE) {
         if (lane == 0) {
@@ -288,7 +281,7 @@ __device__ __forceinline__ RowSums row_sums(RowShared &sh, const Row &row, const
             sh.top[wave] = top;
             if (TWO) {
                 sh.valid[wave] = valid;
-                sh.seen[wave] = seen ? 1u : 0u;
+                sh.seen[wave] = seen;
             }
             if (wave == 0) sh.x = x;   // (read before a wavefront may write there)
         }
@@ -298,11 +291,11 @@ __device__ __forceinline__ RowSums row_sums(RowShared &sh, const Row &row, const
         top = wave_max(sh.top[i]);
         if (TWO) {
             valid = over_lanes<W>(lane < nw ? sh.valid[i] : no_run());
-            seen = __ballot(sh.seen[i] != 0u) != 0ull;
+            seen = (__ballot(sh.seen[i] != 0u) ? 1u : 0u) | (__ballot(sh.seen[i] & LOST) ? LOST : 0u);
         }
         x = sh.x;
     }
-    const bool far = fabsf(top) < INFINITY && (fabsf(top * c) >= FAR_OFF || (TWO && seen && valid.s == 0.f));
+    const bool far = fabsf(top) < INFINITY && (fabsf(top * c) >= FAR_OFF || (TWO && ((seen && valid.s == 0.f) || (seen & LOST))));
     RowSums r;
     r.x = x;
     if (__builtin_expect(__builtin_amdgcn_readfirstlane(far), 0)) {   // (the same for all wavefronts of the row)
@@ -365,18 +358,20 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = ONE ? 1 : blockDim.x / WAVE;
     const int per = ONE ? SHORT_ROWS : 1, first = ONE ? 0 : wave;
     const float step = RAISE * __builtin_amdgcn_rcpf(tp.c);
-    for (int64_t b = (int64_t)blockIdx.x * per + (ONE ? wave : 0); b < B; b += (int64_t)gridDim.x * per) {
+    const int64_t b = (int64_t)blockIdx.x * per + (ONE ? wave : 0);
+    if (b < B) {
         const int tok = tokens ? tokens[b] : V;
         if (tok < 0) {   // left out
             if (lane == 0 && first == 0) {
                 put_values(out, b, {0.f, 0.f, 0.f});
                 if (out.stats) put_stats(out.stats, b, {0.f, 0.f, 0.f}, {0.f, 0.f, 0.f}, {0.f, 0.f, 0.f});
             }
-            continue;
+            return;
         }
         const T *at = logits + b * row_stride;
-        const Row row = row_of(at, V), mrow = MASK ? mask_of(mask, b, n_words) : row;
-        const float x = first == 0 ? logit_of(at, MASK ? mask + b * n_words : nullptr, tok, V) : 0.f;
+        const Row row = row_of(at, V);
+        const uint32_t *mrow = MASK ? mask + b * n_words : nullptr;
+        const float x = first == 0 ? logit_of(at, mrow, tok, V) : 0.f;
         Tally a = no_tally();
         take_tiles<T, MASK, W>(row, mrow, V, share_of(tiles_in<T>(V), first, nw), 0, lane, tp.c, step, a);
         const RowSums r = row_sums<T, MASK, W, ONE>(sh, row, mrow, V, a, x, first, nw, lane, tp.c);
@@ -385,7 +380,6 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
             put_values(out, b, v);
             if (out.stats) put_stats(out.stats, b, r.all, r.q, v);
         }
-        if (!ONE) __syncthreads();   // before LDS is used again
     }
 }
 
@@ -427,13 +421,15 @@ template <bool MASK> __device__ __forceinline__ Slope slope_of(const Sums &all, 
 }
 // Values of this lane's tokens from token v on, rounded to the nearest of their type, once.  What lies behind the row is left as it is.
 __device__ __forceinline__ void put_group(float *row, int v, int V, const float (&d)[4]) {
-    if (v + 4 <= V) {
+    int left = V - v;
+    asm volatile("" : "+v"(left));   // (see unpack_group)
+    if (left >= 4) {
         *(float4 *)(row + v) = {d[0], d[1], d[2], d[3]};
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int k = 0; k < 4; k++)
-        if (v + k < V) row[v + k] = d[k];
+        for (int k = 0; k < 3; k++)
+            if (k < left) row[v + k] = d[k];
+    }
 }
 __device__ __forceinline__ void put_group(uint16_t *row, int v, int V, const float (&d)[8]) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -441,13 +437,15 @@ __device__ __forceinline__ void put_group(uint16_t *row, int v, int V, const flo
     u32x4 r;
 #pragma unroll
     for (int i = 0; i < 4; i++) r[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){d[2 * i], d[2 * i + 1]}, bf16x2));
-    if (v + 8 <= V) {
+    int left = V - v;
+    asm volatile("" : "+v"(left));
+    if (left >= 8) {
         *(u32x4 *)(row + v) = r;
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int k = 0; k < 8; k++)
-        if (v + k < V) row[v + k] = (uint16_t)(r[k / 2] >> (16 * (k & 1)));
+        for (int k = 0; k < 7; k++)
+            if (k < left) row[v + k] = (uint16_t)(r[k / 2] >> (16 * (k & 1)));
+    }
 }
 template <bool FAR> __device__ __forceinline__ float exponent(float x, float r, float c) { return FAR ? (x - r) * c : fmaf(x, c, -r); }
 template <typename T, bool MASK, bool H, bool FAR>
@@ -497,12 +495,13 @@ template <typename T> __device__ __forceinline__ void put_zeros(T *out, int firs
 }
 // The wavefront's tiles from its i-th on; each is read before another one is written: out may be the logits themselves.
 template <typename T, bool MASK, bool H>
-__device__ __forceinline__ void put_tiles(T *out, const Row &row, const Row &mask, const Slope &s, int tok, int V, const Share &share, int i, int lane, float c) {
+__device__ __forceinline__ void put_tiles(T *out, const Row &row, const uint32_t *mask, const Slope &s, int tok, int V, const Share &share, int i, int lane, float c) {
     if (i >= share.n) return;
     MaskedTile<T, MASK> now, next;
-    now.load(row, mask, share.at(i), lane);
+    now.load(row, mask, share.at(i), lane, V);
     for (; i < share.n; i++) {
-        next.load(row, mask, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane);
+        next.load(row, mask, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane, V);
+        now.settle(share.at(i), lane, V);
         put_tile<T, MASK, H>(out, now, s, share.at(i), lane, tok, V, c);
         now = next;
     }
@@ -516,7 +515,8 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void gra
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = blockDim.x / WAVE;
     const int64_t units = ONE ? B : (int64_t)B * parts;
     const int per = ONE ? SHORT_ROWS : 1;
-    for (int64_t u = (int64_t)blockIdx.x * per + (ONE ? wave : 0); u < units; u += (int64_t)gridDim.x * per) {
+    const int64_t u = (int64_t)blockIdx.x * per + (ONE ? wave : 0);
+    if (u < units) {
         const int64_t b = ONE ? u : u / parts;
         const int part = ONE ? 0 : (int)(u - b * parts);
         const int tok = tokens ? tokens[b] : V;
@@ -527,14 +527,14 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void gra
         const int first = ONE ? 0 : part * nw + wave, of = ONE ? 1 : nw * parts;
         if (s.nothing) {
             put_zeros(to, first, of, lane, V);
-            continue;
+            return;
         }
         const Row row = row_of(logits + b * row_stride, V);
-        put_tiles<T, MASK, H>(to, row, MASK ? mask_of(mask, b, n_words) : row, s, tok, V, share_of(tiles_in<T>(V), first, of), 0, lane, tp.c);
+        put_tiles<T, MASK, H>(to, row, MASK ? mask + b * n_words : nullptr, s, tok, V, share_of(tiles_in<T>(V), first, of), 0, lane, tp.c);
     }
 }
 
-// Both: the sums, then the gradient.  A wavefront holds its first HELD tiles; what is more is read again, from cache.
+// Both: the sums, then the gradient.  A wavefront holds its tiles, at most HELD; HELD = 0: they are read again.
 template <typename T, bool MASK, bool W, bool ONE, int HELD>
 __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void score_gradient_kernel(const T *logits, int64_t row_stride, const int32_t *__restrict__ tokens,
                                                                                                   const uint32_t *__restrict__ mask, int V, int n_words, int B,
@@ -543,26 +543,31 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = ONE ? 1 : blockDim.x / WAVE;
     const int per = ONE ? SHORT_ROWS : 1, first = ONE ? 0 : wave;
     const float step = RAISE * __builtin_amdgcn_rcpf(tp.c);
-    for (int64_t b = (int64_t)blockIdx.x * per + (ONE ? wave : 0); b < B; b += (int64_t)gridDim.x * per) {
+    const int64_t b = (int64_t)blockIdx.x * per + (ONE ? wave : 0);
+    if (b < B) {
         const int tok = tokens ? tokens[b] : V;
         T *to = d_logits + b * d_row_stride;
         if (tok < 0) {   // left out
             if (lane == 0 && first == 0) put_values(out, b, {0.f, 0.f, 0.f});
             put_zeros(to, first, nw, lane, V);
-            continue;
+            return;
         }
         const T *at = logits + b * row_stride;
-        const Row row = row_of(at, V), mrow = MASK ? mask_of(mask, b, n_words) : row;
+        const Row row = row_of(at, V);
+        const uint32_t *mrow = MASK ? mask + b * n_words : nullptr;
         const Share share = share_of(tiles_in<T>(V), first, nw);
-        MaskedTile<T, MASK> held[HELD];
+        MaskedTile<T, MASK> held[HELD ? HELD : 1];
 #pragma unroll
-        for (int i = 0; i < HELD; i++) held[i].load(row, mrow, i < share.n ? share.at(i) : NO_TILE, lane);
-        const float x = first == 0 ? logit_of(at, MASK ? mask + b * n_words : nullptr, tok, V) : 0.f;
+        for (int i = 0; i < HELD; i++) held[i].load(row, mrow, i < share.n ? share.at(i) : NO_TILE, lane, V);
+        const float x = first == 0 ? logit_of(at, mrow, tok, V) : 0.f;
         Tally a = no_tally();
 #pragma unroll
         for (int i = 0; i < HELD; i++)
-            if (i < share.n) take_tile<T, MASK, W>(held[i], share.at(i), V, lane, tp.c, step, a);
-        take_tiles<T, MASK, W>(row, mrow, V, share, HELD, lane, tp.c, step, a);
+            if (i < share.n) {
+                held[i].settle(share.at(i), lane, V);
+                take_tile<T, MASK, W>(held[i], share.at(i), V, lane, tp.c, step, a);
+            }
+        if (HELD == 0) take_tiles<T, MASK, W>(row, mrow, V, share, 0, lane, tp.c, step, a);
         const RowSums r = row_sums<T, MASK, W, ONE>(sh, row, mrow, V, a, x, first, nw, lane, tp.c);
         const RowValues v = row_values<MASK>(r.all, r.q, r.x, tp);
         if (lane == 0 && first == 0) put_values(out, b, v);
@@ -573,9 +578,8 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
 #pragma unroll
             for (int i = 0; i < HELD; i++)
                 if (i < share.n) put_tile<T, MASK, W>(to, held[i], s, share.at(i), lane, tok, V, tp.c);
-            put_tiles<T, MASK, W>(to, row, mrow, s, tok, V, share, HELD, lane, tp.c);
+            if (HELD == 0) put_tiles<T, MASK, W>(to, row, mrow, s, tok, V, share, 0, lane, tp.c);
         }
-        if (!ONE) __syncthreads();   // before LDS is used again
     }
 }
 
@@ -610,11 +614,12 @@ struct TopShared {
 };
 // every candidate of the row, one lane and one token at a time: f(key)
 template <typename T, bool MASK, typename F>
-__device__ __forceinline__ void each_candidate(const Row &row, const Row &mask, int V, int first, int step, int lane, F f) {
+__device__ __forceinline__ void each_candidate(const Row &row, const uint32_t *mask, int V, int first, int step, int lane, F f) {
     using G = TileGeom<T>;
     for (int t = first; t * G::TILE < V; t += step) {
         MaskedTile<T, MASK> mt;
-        mt.load(row, mask, t, lane);
+        mt.load(row, mask, t, lane, V);
+        mt.settle(t, lane, V);
 #pragma unroll
         for (int j = 0; j < 4; j++) {
             float x[G::EPL];
@@ -632,7 +637,7 @@ __device__ __forceinline__ void each_candidate(const Row &row, const Row &mask, 
 // The k largest keys of a row into sh.list, in any order; sh.n: how many there are.  Digit by digit from the top: how many candidates
 // have each value of the digit below the digits settled so far, and in which of them the k-th largest lies.  By all wavefronts.
 template <typename T, bool MASK>
-__device__ __forceinline__ void select_row(TopShared &sh, const Row &row, const Row &mask, int V, int k, int wave, int nw, int lane) {
+__device__ __forceinline__ void select_row(TopShared &sh, const Row &row, const uint32_t *mask, int V, int k, int wave, int nw, int lane) {
     const int tid = wave * WAVE + lane;
     if (tid == 0) {
         sh.prefix = 0;
@@ -751,7 +756,8 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
     __shared__ TopShared sh;
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = blockDim.x / WAVE;
     const float step = RAISE * __builtin_amdgcn_rcpf(tp.c);
-    for (int64_t b = blockIdx.x; b < B; b += gridDim.x) {
+    {
+        const int64_t b = blockIdx.x;
         const int tok = tokens ? tokens[b] : V;
         int32_t *ids = top_ids + b * k;
         float *lps = top_logprobs + b * k;
@@ -761,20 +767,22 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
                 ids[i] = -1;
                 lps[i] = -INFINITY;
             }
-            continue;
+            return;
         }
         const T *at = logits + b * row_stride;
-        const Row row = row_of(at, V), mrow = MASK ? mask_of(mask, b, n_words) : row;
-        const float x = wave == 0 ? logit_of(at, MASK ? mask + b * n_words : nullptr, tok, V) : 0.f;
+        const Row row = row_of(at, V);
+        const uint32_t *mrow = MASK ? mask + b * n_words : nullptr;
+        const float x = wave == 0 ? logit_of(at, mrow, tok, V) : 0.f;
         const Share share = share_of(tiles_in<T>(V), wave, nw);
         Tally a = no_tally();
         Best best = {-INFINITY, -INFINITY, 0};
         {
             MaskedTile<T, MASK> now, next;
-            now.load(row, mrow, share.n ? share.at(0) : NO_TILE, lane);
+            now.load(row, mrow, share.n ? share.at(0) : NO_TILE, lane, V);
             for (int i = 0; i < share.n; i++) {
-                next.load(row, mrow, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane);
+                next.load(row, mrow, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane, V);
                 const int tile = share.at(i), left = tokens_left<T>(V, tile, lane);
+                now.settle(tile, lane, V);
                 if ((tile + 1) * G::TILE <= V) top_tile_as<T, MASK, W, false>(now, i, left, lane, tp.c, step, a, best);
                 else top_tile_as<T, MASK, W, true>(now, i, left, lane, tp.c, step, a, best);
                 now = next;
@@ -808,7 +816,7 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
         auto look = [&](int i, int l) __attribute__((always_inline)) {   // at lane l's group i
             const int v = share.at(i >> 2) * G::TILE + (i & 3) * G::PER_LOAD + l * G::EPL;
             list_group<T>(sh, __builtin_amdgcn_raw_buffer_load_b128(row.buf, (uint32_t)v * (uint32_t)sizeof(T), 0, 0),
-                          MASK ? bits_fix<T>(__builtin_amdgcn_raw_buffer_load_b8(mrow.buf, (uint32_t)v >> 3, 0, 0), l) : 0xFFu, v, V, bound);
+                          MASK ? bits_at<T>(mrow, v, V) : 0xFFu, v, V, bound);
         };
         if (mine >= bound && !more) look(best.at, lane);
         // lanes with more than one such group: all of theirs are looked at again, one lane's by the whole wavefront or each its own
@@ -841,33 +849,37 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
                 lps[place] = row_values<false>(r.q, r.q, logit_at((uint32_t)(key >> TOKEN_BITS)), tp).logprob;
             }
         }
-        __syncthreads();   // before LDS is used again
     }
 }
 
 // ------------------------------------------------------------------------------------------
 // Host side.
-struct Shape {
-    unsigned grid, block;
-    bool one;   // rows of one tile
-};
 int tiles_of(int V, ppv_dtype dt) {
     const int tile = dt == PPV_F32 ? TileGeom<float>::TILE : TileGeom<uint16_t>::TILE;
     return (V + tile - 1) / tile;
 }
 // Wavefronts per row: a power of two, at most one per tile.
 int waves_of(int nt, int64_t rows) {
-    const int cap = rows <= 256 ? 16 : (nt >= 48 || rows <= 512 ? 8 : 4);
+    int cap = rows <= 256 ? 16 : (nt >= 48 || rows <= 512 ? 8 : 4);
+    if (const int v = ppv_tuning(PPV_TUNE_WAVES_PER_ROW)) cap = v;
     int nw = 1;
     while (nw < nt && nw * 2 <= cap) nw <<= 1;
     return nw;
 }
-unsigned groups_of(int64_t n) { return (unsigned)(n < (int64_t)MOST_GROUPS ? n : (int64_t)MOST_GROUPS); }
+// How many rows a launch takes: a grid has fewer than 2^32 threads.
+constexpr int64_t MOST_ROWS = 1 << 21;
+struct Shape {
+    unsigned block;
+    int per;    // rows to a workgroup
+    bool one;   // rows of one tile
+    unsigned groups(int64_t rows) const { return (unsigned)((rows + per - 1) / per); }
+};
 Shape shape_of(int V, ppv_dtype dt, int B) {
     const int nt = tiles_of(V, dt);
-    if (nt == 1) return {groups_of(((int64_t)B + SHORT_ROWS - 1) / SHORT_ROWS), SHORT_ROWS * WAVE, true};
-    return {groups_of(B), (unsigned)waves_of(nt, B) * WAVE, false};
+    if (nt == 1) return {SHORT_ROWS * WAVE, SHORT_ROWS, true};
+    return {(unsigned)waves_of(nt, B) * WAVE, 1, false};
 }
+template <typename P> P *from_row(P *p, int64_t b, int64_t stride = 1) { return p ? p + b * stride : nullptr; }
 
 ppv_status check_row_args(const void *logits, ppv_dtype dt, int64_t row_stride, int32_t B, int32_t V, float temperature, Temper *tp) {
     if (B < 0 || !temper_for(temperature, tp)) return PPV_EINVAL;
@@ -904,6 +916,76 @@ ppv_status check_gradient_args(const void *logits, ppv_dtype dt, int64_t row_str
             }                                               \
         }                                                   \
     } while (0)
+#define PPV_LAUNCH(KERNEL, ...) hipLaunchKernelGGL(KERNEL, dim3(grid), dim3(block), 0, hs, __VA_ARGS__)
+
+// A call's rows from row b on, `rows` of them.
+struct Rows {
+    int64_t at;
+    int n, V, n_words;
+    int64_t stride;
+    const void *logits;
+    const uint32_t *mask;
+    const int32_t *tokens;
+    hipStream_t stream;
+    template <typename T> const T *logits_as() const { return (const T *)logits + at * stride; }
+    const uint32_t *mask_rows() const { return from_row(mask, at, n_words); }
+    const int32_t *token_rows() const { return from_row(tokens, at); }
+};
+Outputs from_row(const Outputs &o, int64_t b) {
+    return {from_row(o.logprobs, b), from_row(o.logZ_valid, b), from_row(o.entropy, b), from_row(o.stats, b, PPV_LOGPROB_STATS)};
+}
+Upstream from_row(const Upstream &u, int64_t b) { return {from_row(u.logprobs, b), from_row(u.logZ_valid, b), from_row(u.entropy, b)}; }
+// launch(rows) for all of a call's rows, MOST_ROWS at a time
+template <typename F> ppv_status in_turns(Rows r, int B, F launch) {
+    for (; r.at < B; r.at += MOST_ROWS) {
+        r.n = (int)(B - r.at < MOST_ROWS ? B - r.at : MOST_ROWS);
+        launch(r);
+        PPV_HIP_TRY(hipGetLastError());
+    }
+    return PPV_OK;
+}
+
+template <typename T, bool MASK, bool W> void launch_score(const Rows &r, const Shape &sh, const Outputs &out, const Temper &tp) {
+    const unsigned grid = sh.groups(r.n), block = sh.block;
+    hipStream_t hs = r.stream;
+    if (sh.one)
+        PPV_LAUNCH((score_kernel<T, MASK, W, true>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, from_row(out, r.at), tp);
+    else
+        PPV_LAUNCH((score_kernel<T, MASK, W, false>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, from_row(out, r.at), tp);
+}
+template <typename T, bool MASK, bool H>
+void launch_gradient(const Rows &r, const Shape &sh, int parts, void *d_logits, int64_t d_stride, const float *stats, const Upstream &up, const Temper &tp) {
+    const unsigned grid = sh.one ? sh.groups(r.n) : (unsigned)r.n * (unsigned)parts, block = sh.block;
+    hipStream_t hs = r.stream;
+    T *d = (T *)d_logits + r.at * d_stride;
+    const float *st = stats + r.at * PPV_LOGPROB_STATS;
+    if (sh.one)
+        PPV_LAUNCH((gradient_kernel<T, MASK, H, true>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, 1, d, d_stride, st, from_row(up, r.at), tp);
+    else
+        PPV_LAUNCH((gradient_kernel<T, MASK, H, false>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, parts, d, d_stride, st, from_row(up, r.at), tp);
+}
+constexpr int MOST_HELD = 4;
+template <typename T, bool MASK, bool W>
+void launch_score_gradient(const Rows &r, const Shape &sh, int held, void *d_logits, int64_t d_stride, const Outputs &out, const Upstream &up, const Temper &tp) {
+    const unsigned grid = sh.groups(r.n), block = sh.block;
+    hipStream_t hs = r.stream;
+    T *d = (T *)d_logits + r.at * d_stride;
+#define PPV_SCORE_GRADIENT(ONE, HELD)                                                                                                   \
+    PPV_LAUNCH((score_gradient_kernel<T, MASK, W, ONE, HELD>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, \
+               r.n, d, d_stride, from_row(out, r.at), from_row(up, r.at), tp)
+    if (sh.one) PPV_SCORE_GRADIENT(true, 1);
+    else if (held > MOST_HELD) PPV_SCORE_GRADIENT(false, 0);
+    else if (held > 2) PPV_SCORE_GRADIENT(false, 4);
+    else PPV_SCORE_GRADIENT(false, 2);
+#undef PPV_SCORE_GRADIENT
+}
+template <typename T, bool MASK, bool W>
+void launch_top(const Rows &r, unsigned block, int k, int32_t *top_ids, float *top_logprobs, const Outputs &out, const Temper &tp) {
+    const unsigned grid = (unsigned)r.n;
+    hipStream_t hs = r.stream;
+    PPV_LAUNCH((top_kernel<T, MASK, W>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, k, top_ids + r.at * k,
+               top_logprobs + r.at * k, from_row(out, r.at), tp);
+}
 
 }  // namespace
 
@@ -916,19 +998,11 @@ extern "C" ppv_status ppv_token_logprobs(const void *logits, ppv_dtype dt, int64
     if ((logprobs && !tokens) || (!logprobs && !logZ_valid && !entropy && !stats) || ((uintptr_t)stats & 15u) != 0) return PPV_EINVAL;
     const Outputs out = {logprobs, logZ_valid, entropy, stats};
     const Shape sh = shape_of(V, dt, B);
-    const int n_words = (V + 31) / 32;
-#define PPV_SCORE(T, MASK, ENTROPY)                                                                                                     \
-    do {                                                                                                                                \
-        if (sh.one)                                                                                                                     \
-            hipLaunchKernelGGL((score_kernel<T, MASK, ENTROPY, true>), dim3(sh.grid), dim3(sh.block), 0, (hipStream_t)stream,           \
-                               (const T *)logits, row_stride, tokens, mask, V, n_words, B, out, tp);                                    \
-        else                                                                                                                            \
-            hipLaunchKernelGGL((score_kernel<T, MASK, ENTROPY, false>), dim3(sh.grid), dim3(sh.block), 0, (hipStream_t)stream,          \
-                               (const T *)logits, row_stride, tokens, mask, V, n_words, B, out, tp);                                    \
-    } while (0)
-    PPV_PICK(dt, mask, entropy || stats, PPV_SCORE);
-    PPV_HIP_TRY(hipGetLastError());
-    return PPV_OK;
+    return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
+#define PPV_CALL(T, MASK, W) launch_score<T, MASK, W>(r, sh, out, tp)
+        PPV_PICK(dt, mask, entropy || stats, PPV_CALL);
+#undef PPV_CALL
+    });
 }
 
 extern "C" ppv_status ppv_token_logprobs_backward(const void *logits, ppv_dtype dt, int64_t row_stride, const uint32_t *mask,
@@ -942,23 +1016,14 @@ extern "C" ppv_status ppv_token_logprobs_backward(const void *logits, ppv_dtype 
     st = check_gradient_args(logits, dt, row_stride, B, V, d_logits, d_row_stride);
     if (st != PPV_OK) return st;
     const Upstream up = {d_logprobs, d_logZ_valid, d_entropy};
-    Shape sh = shape_of(V, dt, B);
-    const int n_words = (V + 31) / 32, nt = tiles_of(V, dt);
+    const Shape sh = shape_of(V, dt, B);
     int parts = 1;
-    while (!sh.one && (int64_t)B * parts < 512 && (int)(sh.block / WAVE) * parts * 2 <= nt) parts *= 2;
-    if (!sh.one) sh.grid = groups_of((int64_t)B * parts);
-#define PPV_GRADIENT(T, MASK, ENTROPY)                                                                                                  \
-    do {                                                                                                                                \
-        if (sh.one)                                                                                                                     \
-            hipLaunchKernelGGL((gradient_kernel<T, MASK, ENTROPY, true>), dim3(sh.grid), dim3(sh.block), 0, (hipStream_t)stream,        \
-                               (const T *)logits, row_stride, tokens, mask, V, n_words, B, 1, (T *)d_logits, d_row_stride, stats, up, tp); \
-        else                                                                                                                            \
-            hipLaunchKernelGGL((gradient_kernel<T, MASK, ENTROPY, false>), dim3(sh.grid), dim3(sh.block), 0, (hipStream_t)stream,       \
-                               (const T *)logits, row_stride, tokens, mask, V, n_words, B, parts, (T *)d_logits, d_row_stride, stats, up, tp); \
-    } while (0)
-    PPV_PICK(dt, mask, d_entropy, PPV_GRADIENT);
-    PPV_HIP_TRY(hipGetLastError());
-    return PPV_OK;
+    while (!sh.one && (int64_t)B * parts < 512 && (int)(sh.block / WAVE) * parts * 2 <= tiles_of(V, dt)) parts *= 2;
+    return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
+#define PPV_CALL(T, MASK, H) launch_gradient<T, MASK, H>(r, sh, parts, d_logits, d_row_stride, stats, up, tp)
+        PPV_PICK(dt, mask, d_entropy, PPV_CALL);
+#undef PPV_CALL
+    });
 }
 
 extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, int64_t row_stride, const uint32_t *mask, const int32_t *tokens,
@@ -973,20 +1038,18 @@ extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, 
     if (st != PPV_OK) return st;
     const Upstream up = {d_logprobs, d_logZ_valid, d_entropy};
     const Outputs out = {logprobs, logZ_valid, entropy, nullptr};
-    const Shape sh = shape_of(V, dt, B);
-    const int n_words = (V + 31) / 32;
-#define PPV_SCORE_GRADIENT(T, MASK, ENTROPY)                                                                                            \
-    do {                                                                                                                                \
-        if (sh.one)                                                                                                                     \
-            hipLaunchKernelGGL((score_gradient_kernel<T, MASK, ENTROPY, true, 1>), dim3(sh.grid), dim3(sh.block), 0, (hipStream_t)stream,  \
-                               (const T *)logits, row_stride, tokens, mask, V, n_words, B, (T *)d_logits, d_row_stride, out, up, tp);   \
-        else                                                                                                                            \
-            hipLaunchKernelGGL((score_gradient_kernel<T, MASK, ENTROPY, false, MASK ? 2 : 4>), dim3(sh.grid), dim3(sh.block), 0, (hipStream_t)stream, \
-                               (const T *)logits, row_stride, tokens, mask, V, n_words, B, (T *)d_logits, d_row_stride, out, up, tp);   \
-    } while (0)
-    PPV_PICK(dt, mask, entropy || d_entropy, PPV_SCORE_GRADIENT);
-    PPV_HIP_TRY(hipGetLastError());
-    return PPV_OK;
+    Shape sh = shape_of(V, dt, B);
+    // enough wavefronts to hold the row, if there are as many
+    const int nt = tiles_of(V, dt);
+    int nw = (int)sh.block / WAVE;
+    while (!sh.one && nw < MOST_WAVES && nt > MOST_HELD * nw) nw *= 2;
+    if (!sh.one) sh.block = (unsigned)nw * WAVE;
+    const int held = (nt + nw - 1) / nw;
+    return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
+#define PPV_CALL(T, MASK, W) launch_score_gradient<T, MASK, W>(r, sh, held, d_logits, d_row_stride, out, up, tp)
+        PPV_PICK(dt, mask, entropy || d_entropy, PPV_CALL);
+#undef PPV_CALL
+    });
 }
 
 extern "C" ppv_status ppv_top_logprobs(const void *logits, ppv_dtype dt, int64_t row_stride, const uint32_t *mask, const int32_t *tokens,
@@ -999,12 +1062,10 @@ extern "C" ppv_status ppv_top_logprobs(const void *logits, ppv_dtype dt, int64_t
     if (st != PPV_OK || B == 0) return st;
     if (!top_ids || !top_logprobs || (logprobs && !tokens)) return PPV_EINVAL;
     const Outputs out = {logprobs, nullptr, entropy, nullptr};
-    const int n_words = (V + 31) / 32;
     const unsigned block = (unsigned)waves_of(tiles_of(V, dt), B) * WAVE;
-#define PPV_TOP(T, MASK, ENTROPY)                                                                                                       \
-    hipLaunchKernelGGL((top_kernel<T, MASK, ENTROPY>), dim3(groups_of(B)), dim3(block), 0, (hipStream_t)stream, (const T *)logits,      \
-                       row_stride, tokens, mask, V, n_words, B, k, top_ids, top_logprobs, out, tp)
-    PPV_PICK(dt, mask, entropy, PPV_TOP);
-    PPV_HIP_TRY(hipGetLastError());
-    return PPV_OK;
+    return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
+#define PPV_CALL(T, MASK, W) launch_top<T, MASK, W>(r, block, k, top_ids, top_logprobs, out, tp)
+        PPV_PICK(dt, mask, entropy, PPV_CALL);
+#undef PPV_CALL
+    });
 }
