@@ -90,6 +90,10 @@ struct SplitScratch {
 // The scratch area for `rows` rows (PPV_SPLIT_MAX_ROWS at most) of a call on this stream of the current device, or of the capture
 // that the stream is in; nullptr when there is none to be had: the rows are then not split.
 SplitScratch *ppv_split_scratch(hipStream_t stream, int rows);
+// A mark for a call that splits rows; without one (not split) 0.  PPV_LOOK_ONCE, of a mark (tests, see ppv_split_look): no further look.
+constexpr uint32_t PPV_LOOK_ONCE = 1u << 29;
+uint32_t ppv_split_mark(int split_shift);
+void ppv_split_look(bool again);
 // The area of eager calls on a stream, or constrained_sample_noalloc's array: its address, its size and where the rows' words begin,
 // for the tests that look at one or disturb it; look_again 0: calls from now on look once at a word.  (Exported, and not declared in
 // ppv.h.)

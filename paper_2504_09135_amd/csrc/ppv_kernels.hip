@@ -23,6 +23,7 @@
 #include "ppv_device.h"
 #include "ppv_internal.h"
 #include "ppv_rows.h"
+#include "ppv_split.h"
 #include "ppv_walk.h"
 
 namespace {
@@ -464,63 +465,6 @@ struct RowOut {
     bool mine;         // this thread holds the row's result (wavefront 0 of the workgroup that finishes the row;
                        // every thread of it with ALL)
 };
-
-// Words that the workgroups of a split row hand to one another (see SplitRow) are written and read with device-scope
-// accesses (each goes to the level of the memory system that all compute units share), so that no fence over the whole
-// cache is needed: a device-wide fence per wavefront cost 30 us per launch.
-template <typename W> __device__ __forceinline__ void shared_put(W *p, W v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-template <typename W> __device__ __forceinline__ W shared_get(const W *p) {
-    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
-// A row shared by `parts` workgroups (see SplitRow); parts == 1: one workgroup has the row to itself and
-// nothing else here is looked at.
-struct Split {
-    int parts;
-    int part;             // this workgroup's number, 0 .. parts-1
-    SplitRow *row;        // the row's scratch
-    uint32_t *arrivals;   // the row's arrival counter
-    uint32_t mark;        // of the call
-};
-template <bool SPLIT> __device__ __forceinline__ Split split_of(int shift) {
-    if (!SPLIT) return {1, 0, nullptr, nullptr, 0u};
-    return {1 << shift, (int)(blockIdx.x & ((1u << shift) - 1u)), nullptr, nullptr, 0u};
-}
-// (Where it is needed, not when the kernel starts: on the way through the index there is no room for it in the scalar registers.)
-template <bool SPLIT> __device__ __forceinline__ void find_area(Split &sp, SplitScratch *scratch, int b, uint32_t mark) {
-    if (!SPLIT) return;
-    sp.row = &scratch->row[b];
-    sp.arrivals = &scratch->arrivals[b];
-    sp.mark = mark;
-}
-__device__ __forceinline__ void send(Marked *p, float v, uint32_t mark) { shared_put(p, (uint64_t)mark << 32 | __float_as_uint(v)); }
-__device__ __forceinline__ void send(MarkedPair *p, float a, float b, uint32_t mark) {
-    send(&p->first, a, mark);
-    send(&p->second, b, mark);
-}
-__device__ __forceinline__ void clear(MarkedPair *p) {
-    shared_put(&p->first, (Marked)0);
-    shared_put(&p->second, (Marked)0);
-}
-__device__ __forceinline__ MarkedPair look(const MarkedPair *p) { return {shared_get(&p->first), shared_get(&p->second)}; }
-__device__ __forceinline__ bool has(Marked w, uint32_t mark) { return (uint32_t)(w >> 32) == mark; }
-__device__ __forceinline__ bool has(const MarkedPair &w, uint32_t mark) { return has(w.first, mark) && has(w.second, mark); }
-__device__ __forceinline__ float value(Marked w) { return __uint_as_float((uint32_t)w); }
-// Waits for words that have been sent, by a whole wavefront: look_again() at all of them as long as one lane's there() is false.  False if they
-// do not come: two launches use one area at a time, which no caller may do.  (The row then has no result, and says so: id -1, masses NaN.)
-constexpr uint32_t MOST_LOOKS = 1u << 16;      // a word that has been sent comes within microseconds
-constexpr uint32_t LOOK_ONCE = 1u << 29;       // of a mark (tests): no further look
-template <typename THERE, typename LOOK> __device__ __forceinline__ bool wait_for(const Split &sp, THERE there, LOOK look_again) {
-    uint32_t n = 0;
-    while (__ballot(!there()) != 0ull) {   // (uniform: what is live here is in scalar registers, of which there are too few)
-        if (n++ >= MOST_LOOKS || (sp.mark & LOOK_ONCE)) return false;
-        look_again();
-    }
-    return true;
-}
-// Counts this workgroup: true for the one that arrives last.  (The count goes from parts - 1 to 0, and from anything that is more: what launches
-// that may not have met here leave in it makes some workgroup of a later one the last, which waits for the words of the others.)
-__device__ __forceinline__ bool arrive(const Split &sp) { return atomicInc(sp.arrivals, (uint32_t)sp.parts - 1u) >= (uint32_t)sp.parts - 1u; }
 
 // Where the workgroups of a row meet: by wavefront 0 of each, after a barrier behind the last word the workgroup has sent.  True for the
 // one that arrives last, which then has every tile's statistics in its LDS; nobody waits for a workgroup that has not arrived.
@@ -2196,22 +2140,13 @@ int shift_of(int parts) {
     return sh;
 }
 
-// A mark for a call that splits rows (see SplitRow); 0 for the others.
-std::atomic<uint32_t> g_mark_flags{0};
-uint32_t mark_for(int split_shift) {
-    static std::atomic<uint32_t> last{0};
-    uint32_t mark = 0;
-    while (split_shift && !mark) mark = ++last & (LOOK_ONCE - 1u);
-    return mark | g_mark_flags.load(std::memory_order_relaxed);
-}
-
 template <typename T>
 void launch_sample(bool small, dim3 grid, dim3 block, hipStream_t hs, const T *lg, int64_t row_stride,
                    const uint32_t *mask, const float *uniforms, int V, int n_words, int list_max, int32_t *ids,
                    float *logZ_valid, float *logZ_all, Temper tp, int split_shift, SplitScratch *scratch) {
 #define PPV_LAUNCH_SAMPLE(SMALL, SPLIT)                                                                                  \
     hipLaunchKernelGGL((sample_kernel<T, SMALL, SPLIT>), grid, block, 0, hs, lg, row_stride, mask, V, n_words, \
-                       list_max, split_shift | (int)(block.x / WAVE) << 8, scratch, uniforms, ids, logZ_valid, logZ_all, tp, mark_for(split_shift))
+                       list_max, split_shift | (int)(block.x / WAVE) << 8, scratch, uniforms, ids, logZ_valid, logZ_all, tp, ppv_split_mark(split_shift))
     if (split_shift) PPV_LAUNCH_SAMPLE(false, true);
     else if (small) PPV_LAUNCH_SAMPLE(true, false);
     else PPV_LAUNCH_SAMPLE(false, false);
@@ -2226,7 +2161,7 @@ void launch_decode_kernel(bool loop, dim3 grid, dim3 block, hipStream_t hs, cons
                           float *logZ_valid, float *logx, Temper tp, int split_shift, SplitScratch *scratch, int flags) {
     const bool reg = rs && (!loop || B <= REG_MAX_ROWS);
 #define PPV_LAUNCH_DECODE(LOOP, SPLIT, REG)                                                                               \
-    hipLaunchKernelGGL((decode_kernel<T, LOOP, SPLIT, REG>), grid, block, 0, hs, active, lens, rs, uniforms, logx, lg, flags | (int)(mark_for(split_shift) << 2), \
+    hipLaunchKernelGGL((decode_kernel<T, LOOP, SPLIT, REG>), grid, block, 0, hs, active, lens, rs, uniforms, logx, lg, flags | (int)(ppv_split_mark(split_shift) << 2), \
                        split_shift | (int)(block.x / WAVE) << 8, prefixes, stride, n_steps, B, row_stride, step_stride, ids,  \
                        logZ_valid, scratch, tp, view)
     if (split_shift && !loop && reg) PPV_LAUNCH_DECODE(false, true, true);
@@ -2339,7 +2274,7 @@ ppv_status ppv_split_area_for_tests(void *stream, int32_t fixed, int32_t look_ag
         if (st != PPV_OK) return st;
     }
     if (!p) return PPV_ENOMEM;
-    g_mark_flags = look_again ? 0u : LOOK_ONCE;
+    ppv_split_look(look_again != 0);
     *area = p;
     *bytes = (int64_t)sizeof(SplitScratch);
     *words_at = (int64_t)offsetof(SplitScratch, row);

@@ -121,6 +121,17 @@ SplitScratch *area_for(hipStream_t stream, int rows) {
 }
 }  // namespace
 
+namespace {
+std::atomic<uint32_t> g_mark_flags{0};
+}
+uint32_t ppv_split_mark(int split_shift) {
+    static std::atomic<uint32_t> last{0};
+    uint32_t mark = 0;
+    while (split_shift && !mark) mark = ++last & (PPV_LOOK_ONCE - 1u);
+    return mark | g_mark_flags.load(std::memory_order_relaxed);
+}
+void ppv_split_look(bool again) { g_mark_flags = again ? 0u : PPV_LOOK_ONCE; }
+
 SplitScratch *ppv_split_scratch(hipStream_t stream, int rows) {
     try {
         return area_for(stream, rows);
