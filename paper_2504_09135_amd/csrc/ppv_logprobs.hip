@@ -9,6 +9,7 @@
 // A row is read once, by all lanes of its wavefronts, each with its own running reference and sums relative to it; the lanes' sums are
 // brought to one reference at the end.  Sums are fp32: a lane adds at most 4,096 terms of one sign.
 #include "ppv_rows.h"
+#include "ppv_split.h"
 
 namespace {
 
@@ -251,53 +252,87 @@ __device__ __forceinline__ void take_row_careful(const Row &row, const uint32_t 
     valid = over_lanes(valid, c);
 }
 
-// What the wavefronts of a workgroup have found, to every one of them.
-struct RowShared {
-    Run all[MOST_WAVES], valid[MOST_WAVES];
-    Sums careful_all[MOST_WAVES], careful_valid[MOST_WAVES];
-    float top[MOST_WAVES];
-    uint32_t seen[MOST_WAVES];
-    float x;   // the row's token's logit
+// What a wavefront, a workgroup or several of them have found in their share of a row.
+struct Part {
+    Run all, valid;   // over all tokens, and over the valid ones (TWO: they are told apart)
+    float top;        // the largest token
+    uint32_t seen;    // 1: there were valid tokens; LOST
 };
+template <bool TWO, bool W> __device__ __forceinline__ Part over_lanes(const Part &p) {
+    return {over_lanes<W && !TWO>(p.all), TWO ? over_lanes<W>(p.valid) : no_run(), wave_max(p.top),
+            TWO ? (__ballot(p.seen != 0u) ? 1u : 0u) | (__ballot(p.seen & LOST) ? LOST : 0u) : 0u};
+}
+__device__ __forceinline__ Part no_part() { return {no_run(), no_run(), -INFINITY, 0u}; }
+
+constexpr int NOT_COME = 2;
+struct RowShared {
+    Part part[MOST_WAVES];
+    Part met;   // of all workgroups of a split row
+    Sums careful_all[MOST_WAVES], careful_valid[MOST_WAVES];
+    float x;    // the row's token's logit
+    int mine;   // this workgroup finishes the row; NOT_COME: without all of the others' words
+};
+// A workgroup's wavefronts' tallies and the token's logit (`x`: known to wavefront 0), to every wavefront.  ONE: there is one.
+template <bool TWO, bool W, bool ONE> __device__ __forceinline__ Part workgroup_part(RowShared &sh, const Tally &a, float &x, int wave, int nw, int lane) {
+    Part p = over_lanes<TWO, W>({a.all, TWO ? both<W>({a.all.r, a.s, a.w}, a.few) : no_run(), a.top, a.seen});
+    if (ONE) return p;
+    if (lane == 0) {
+        sh.part[wave] = p;
+        if (wave == 0) sh.x = x;   // (read before a wavefront may write there)
+    }
+    __syncthreads();
+    x = sh.x;
+    return over_lanes<TWO, W>(lane < nw ? sh.part[lane] : no_part());
+}
+
+// A split row's workgroups hand over their parts as words of the row's scratch, PART_WORDS each.  (by wavefront 0)
+constexpr int PART_WORDS = 8;
+static_assert(PPV_SPLIT_MAX_PARTS * PART_WORDS == 2 * WAVE, "two words a lane");
+__device__ __forceinline__ void send_part(const Split &sp, const Part &p, int lane) {
+    const float words[PART_WORDS] = {p.all.r, p.all.s, p.all.w, p.valid.r, p.valid.s, p.valid.w, p.top, __uint_as_float(p.seen)};
+    float v = words[0];
+#pragma unroll
+    for (int i = 1; i < PART_WORDS; i++) v = lane == i ? words[i] : v;
+    if (lane < PART_WORDS) send((Marked *)sp.row + sp.part * PART_WORDS + lane, v, sp.mark);
+}
+struct PartWords {
+    Marked a, b;
+};
+__device__ __forceinline__ PartWords look_at_parts(const Split &sp, int lane) {   // (no lane without a word: conditions are registers)
+    const Marked *at = (const Marked *)sp.row;
+    const int n = sp.parts * PART_WORDS;
+    return {shared_get(at + min(lane, n - 1)), shared_get(at + min(lane + WAVE, n - 1))};
+}
+// The parts of all workgroups, once they have arrived.  Words that do not come leave NaN.
+template <bool TWO, bool W> __device__ __forceinline__ Part receive_parts(const Split &sp, PartWords w, int lane) {
+    const bool come = wait_for(sp, [&]() __attribute__((always_inline)) { return has(w.a, sp.mark) && has(w.b, sp.mark); },
+                               [&]() __attribute__((always_inline)) { w = look_at_parts(sp, lane); });
+    Marked *at = (Marked *)sp.row;
+    const int n = sp.parts * PART_WORDS;
+    if (lane < n) shared_put(at + lane, (Marked)0);   // (for a graph, all of whose replays have one mark)
+    if (lane + WAVE < n) shared_put(at + lane + WAVE, (Marked)0);
+    float v[PART_WORDS];
+#pragma unroll
+    for (int i = 0; i < PART_WORDS; i++) {   // lane l: part l
+        const int from = (lane & 7) * PART_WORDS + i;
+        const float a = __shfl(value(w.a), from, WAVE), b = __shfl(value(w.b), from, WAVE);
+        v[i] = lane < 8 ? a : b;
+    }
+    Part p = over_lanes<TWO, W>(lane < sp.parts ? Part{{v[0], v[1], v[2]}, {v[3], v[4], v[5]}, v[6], __float_as_uint(v[7])} : no_part());
+    if (!come) p.all.s = p.valid.s = __uint_as_float(0x7FC00000u);
+    return p;
+}
+
 struct RowSums {
     Sums all, q;   // over all tokens, and over the valid ones
-    float x;       // the row's token's logit
 };
-// `x`: known to wavefront 0.  By every wavefront of the row (ONE: the only one).  ONLY: the tally is of the valid tokens alone, and so is the
-// result.
-template <typename T, bool MASK, bool W, bool ONE, bool ONLY = false>
-__device__ __forceinline__ RowSums row_sums(RowShared &sh, const Row &row, const uint32_t *mask, int V, const Tally &a, float x, int wave, int nw, int lane, float c) {
-    constexpr bool TWO = MASK && !ONLY;   // two sets of sums
-    Run all = over_lanes<W && !TWO>(a.all), valid = no_run();
-    float top = wave_max(a.top);
-    uint32_t seen = 0u;
-    if (TWO) {
-        valid = over_lanes<W>(both<W>({a.all.r, a.s, a.w}, a.few));
-        seen = (__ballot(a.seen != 0u) ? 1u : 0u) | (__ballot(a.seen & LOST) ? LOST : 0u);
-    }
-    if (!ONE) {
-        if (lane == 0) {
-            sh.all[wave] = all;
-            sh.top[wave] = top;
-            if (TWO) {
-                sh.valid[wave] = valid;
-                sh.seen[wave] = seen;
-            }
-            if (wave == 0) sh.x = x;   // (read before a wavefront may write there)
-        }
-        __syncthreads();
-        const int i = lane < nw ? lane : 0;
-        all = over_lanes<W && !TWO>(lane < nw ? sh.all[i] : no_run());
-        top = wave_max(sh.top[i]);
-        if (TWO) {
-            valid = over_lanes<W>(lane < nw ? sh.valid[i] : no_run());
-            seen = (__ballot(sh.seen[i] != 0u) ? 1u : 0u) | (__ballot(sh.seen[i] & LOST) ? LOST : 0u);
-        }
-        x = sh.x;
-    }
-    const bool far = fabsf(top) < INFINITY && (fabsf(top * c) >= FAR_OFF || (TWO && ((seen && valid.s == 0.f) || (seen & LOST))));
+// By every wavefront of the workgroup that has the row's part (ONE: the only one).  ONLY: the part is of the valid tokens alone, and so is
+// the result.
+template <typename T, bool MASK, bool ONE, bool ONLY = false>
+__device__ __forceinline__ RowSums row_sums(RowShared &sh, const Row &row, const uint32_t *mask, int V, const Part &p, int wave, int nw, int lane, float c) {
+    constexpr bool TWO = MASK && !ONLY;
+    const bool far = fabsf(p.top) < INFINITY && (fabsf(p.top * c) >= FAR_OFF || (TWO && ((p.seen && p.valid.s == 0.f) || (p.seen & LOST))));
     RowSums r;
-    r.x = x;
     if (__builtin_expect(__builtin_amdgcn_readfirstlane(far), 0)) {   // (the same for all wavefronts of the row)
         take_row_careful<T, MASK>(row, mask, V, wave, nw, lane, c, r.all, r.q);
         if (!ONE) {
@@ -312,8 +347,8 @@ __device__ __forceinline__ RowSums row_sums(RowShared &sh, const Row &row, const
         if (!MASK) r.q = r.all;
         return r;
     }
-    r.all = sums_of(all, c);
-    r.q = TWO ? sums_of(valid, c) : r.all;
+    r.all = sums_of(p.all, c);
+    r.q = TWO ? sums_of(p.valid, c) : r.all;
     return r;
 }
 
@@ -349,37 +384,55 @@ __device__ __forceinline__ void put_values(const Outputs &o, int64_t b, const Ro
 }
 
 // ------------------------------------------------------------------------------------------
-// Forward.  ONE: rows of one tile, a wavefront each; else a workgroup has a row.
-template <typename T, bool MASK, bool W, bool ONE>
+// Forward.  ONE: rows of one tile, a wavefront each; else a workgroup has a row, or (SPLIT) 1 << shift of them have.
+template <typename T, bool MASK, bool W, bool ONE, bool SPLIT>
 __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void score_kernel(const T *__restrict__ logits, int64_t row_stride,
                                                                                          const int32_t *__restrict__ tokens, const uint32_t *__restrict__ mask,
-                                                                                         int V, int n_words, int B, Outputs out, Temper tp) {
+                                                                                         int V, int n_words, int B, int shift, SplitScratch *scratch, uint32_t mark,
+                                                                                         Outputs out, Temper tp) {
     __shared__ RowShared sh;
-    const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = ONE ? 1 : blockDim.x / WAVE;
-    const int per = ONE ? SHORT_ROWS : 1, first = ONE ? 0 : wave;
-    const float step = RAISE * __builtin_amdgcn_rcpf(tp.c);
-    const int64_t b = (int64_t)blockIdx.x * per + (ONE ? wave : 0);
-    if (b < B) {
-        const int tok = tokens ? tokens[b] : V;
-        if (tok < 0) {   // left out
-            if (lane == 0 && first == 0) {
-                put_values(out, b, {0.f, 0.f, 0.f});
-                if (out.stats) put_stats(out.stats, b, {0.f, 0.f, 0.f}, {0.f, 0.f, 0.f}, {0.f, 0.f, 0.f});
+    const int lane = threadIdx.x & (WAVE - 1), wave = ONE ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = ONE ? 1 : blockDim.x / WAVE;
+    const int64_t b = ONE ? (int64_t)blockIdx.x * SHORT_ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) : blockIdx.x >> (SPLIT ? shift : 0);
+    if (ONE && b >= B) return;
+    Split sp = split_of<SPLIT>(shift);
+    const int tok = tokens ? tokens[b] : V;
+    if (tok < 0) {   // left out
+        if (lane == 0 && wave == 0 && sp.part == 0) {
+            put_values(out, b, {0.f, 0.f, 0.f});
+            if (out.stats) put_stats(out.stats, b, {0.f, 0.f, 0.f}, {0.f, 0.f, 0.f}, {0.f, 0.f, 0.f});
+        }
+        return;
+    }
+    const T *at = logits + b * row_stride;
+    const Row row = row_of(at, V);
+    const uint32_t *mrow = MASK ? mask + b * n_words : nullptr;
+    float x = wave == 0 ? logit_of(at, mrow, tok, V) : 0.f;
+    Tally a = no_tally();
+    take_tiles<T, MASK, W>(row, mrow, V, share_of(tiles_in<T>(V), sp.part * nw + wave, sp.parts * nw), 0, lane, tp.c, RAISE * __builtin_amdgcn_rcpf(tp.c), a);
+    Part p = workgroup_part<MASK, W, ONE>(sh, a, x, wave, nw, lane);
+    if (SPLIT) {
+        if (wave == 0) {
+            find_area<SPLIT>(sp, scratch, (int)b, mark);
+            send_part(sp, p, lane);
+            const PartWords w = look_at_parts(sp, lane);
+            int last = 0;
+            if (lane == 0) last = arrive(sp) ? 1 : 0;
+            last = __builtin_amdgcn_readfirstlane(last);
+            if (last) {
+                p = receive_parts<MASK, W>(sp, w, lane);
+                if (lane == 0) sh.met = p;
             }
-            return;
+            if (lane == 0) sh.mine = last;
         }
-        const T *at = logits + b * row_stride;
-        const Row row = row_of(at, V);
-        const uint32_t *mrow = MASK ? mask + b * n_words : nullptr;
-        const float x = first == 0 ? logit_of(at, mrow, tok, V) : 0.f;
-        Tally a = no_tally();
-        take_tiles<T, MASK, W>(row, mrow, V, share_of(tiles_in<T>(V), first, nw), 0, lane, tp.c, step, a);
-        const RowSums r = row_sums<T, MASK, W, ONE>(sh, row, mrow, V, a, x, first, nw, lane, tp.c);
-        if (lane == 0 && first == 0) {
-            const RowValues v = row_values<MASK>(r.all, r.q, r.x, tp);
-            put_values(out, b, v);
-            if (out.stats) put_stats(out.stats, b, r.all, r.q, v);
-        }
+        __syncthreads();
+        if (!sh.mine) return;
+        p = sh.met;
+    }
+    const RowSums r = row_sums<T, MASK, ONE>(sh, row, mrow, V, p, wave, nw, lane, tp.c);
+    if (lane == 0 && wave == 0) {
+        const RowValues v = row_values<MASK>(r.all, r.q, x, tp);
+        put_values(out, b, v);
+        if (out.stats) put_stats(out.stats, b, r.all, r.q, v);
     }
 }
 
@@ -540,47 +593,46 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
                                                                                                   const uint32_t *__restrict__ mask, int V, int n_words, int B,
                                                                                                   T *d_logits, int64_t d_row_stride, Outputs out, Upstream up, Temper tp) {
     __shared__ RowShared sh;
-    const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = ONE ? 1 : blockDim.x / WAVE;
-    const int per = ONE ? SHORT_ROWS : 1, first = ONE ? 0 : wave;
-    const float step = RAISE * __builtin_amdgcn_rcpf(tp.c);
-    const int64_t b = (int64_t)blockIdx.x * per + (ONE ? wave : 0);
-    if (b < B) {
-        const int tok = tokens ? tokens[b] : V;
-        T *to = d_logits + b * d_row_stride;
-        if (tok < 0) {   // left out
-            if (lane == 0 && first == 0) put_values(out, b, {0.f, 0.f, 0.f});
-            put_zeros(to, first, nw, lane, V);
-            return;
-        }
-        const T *at = logits + b * row_stride;
-        const Row row = row_of(at, V);
-        const uint32_t *mrow = MASK ? mask + b * n_words : nullptr;
-        const Share share = share_of(tiles_in<T>(V), first, nw);
-        MaskedTile<T, MASK> held[HELD ? HELD : 1];
-#pragma unroll
-        for (int i = 0; i < HELD; i++) held[i].load(row, mrow, i < share.n ? share.at(i) : NO_TILE, lane, V);
-        const float x = first == 0 ? logit_of(at, mrow, tok, V) : 0.f;
-        Tally a = no_tally();
-#pragma unroll
-        for (int i = 0; i < HELD; i++)
-            if (i < share.n) {
-                held[i].settle(share.at(i), lane, V);
-                take_tile<T, MASK, W>(held[i], share.at(i), V, lane, tp.c, step, a);
-            }
-        if (HELD == 0) take_tiles<T, MASK, W>(row, mrow, V, share, 0, lane, tp.c, step, a);
-        const RowSums r = row_sums<T, MASK, W, ONE>(sh, row, mrow, V, a, x, first, nw, lane, tp.c);
-        const RowValues v = row_values<MASK>(r.all, r.q, r.x, tp);
-        if (lane == 0 && first == 0) put_values(out, b, v);
-        const Slope s = slope_of<MASK>(r.all, r.q, v.entropy, v.logprob, up, b, tok, tp);
-        if (s.nothing) {
-            put_zeros(to, first, nw, lane, V);
-        } else {
-#pragma unroll
-            for (int i = 0; i < HELD; i++)
-                if (i < share.n) put_tile<T, MASK, W>(to, held[i], s, share.at(i), lane, tok, V, tp.c);
-            if (HELD == 0) put_tiles<T, MASK, W>(to, row, mrow, s, tok, V, share, 0, lane, tp.c);
-        }
+    const int lane = threadIdx.x & (WAVE - 1), wave = ONE ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = ONE ? 1 : blockDim.x / WAVE;
+    const int64_t b = ONE ? (int64_t)blockIdx.x * SHORT_ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) : blockIdx.x;
+    if (ONE && b >= B) return;
+    const int tok = tokens ? tokens[b] : V;
+    T *to = d_logits + b * d_row_stride;
+    if (tok < 0) {   // left out
+        if (lane == 0 && wave == 0) put_values(out, b, {0.f, 0.f, 0.f});
+        put_zeros(to, wave, nw, lane, V);
+        return;
     }
+    const T *at = logits + b * row_stride;
+    const Row row = row_of(at, V);
+    const uint32_t *mrow = MASK ? mask + b * n_words : nullptr;
+    const Share share = share_of(tiles_in<T>(V), wave, nw);
+    MaskedTile<T, MASK> held[HELD ? HELD : 1];
+#pragma unroll
+    for (int i = 0; i < HELD; i++) held[i].load(row, mrow, i < share.n ? share.at(i) : NO_TILE, lane, V);
+    float x = wave == 0 ? logit_of(at, mrow, tok, V) : 0.f;
+    const float step = RAISE * __builtin_amdgcn_rcpf(tp.c);
+    Tally a = no_tally();
+#pragma unroll
+    for (int i = 0; i < HELD; i++)
+        if (i < share.n) {
+            held[i].settle(share.at(i), lane, V);
+            take_tile<T, MASK, W>(held[i], share.at(i), V, lane, tp.c, step, a);
+        }
+    if (HELD == 0) take_tiles<T, MASK, W>(row, mrow, V, share, 0, lane, tp.c, step, a);
+    const Part p = workgroup_part<MASK, W, ONE>(sh, a, x, wave, nw, lane);
+    const RowSums r = row_sums<T, MASK, ONE>(sh, row, mrow, V, p, wave, nw, lane, tp.c);
+    const RowValues v = row_values<MASK>(r.all, r.q, x, tp);
+    if (lane == 0 && wave == 0) put_values(out, b, v);
+    const Slope s = slope_of<MASK>(r.all, r.q, v.entropy, v.logprob, up, b, tok, tp);
+    if (s.nothing) {
+        put_zeros(to, wave, nw, lane, V);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < HELD; i++)
+        if (i < share.n) put_tile<T, MASK, W>(to, held[i], s, share.at(i), lane, tok, V, tp.c);
+    if (HELD == 0) put_tiles<T, MASK, W>(to, row, mrow, s, tok, V, share, 0, lane, tp.c);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -634,10 +686,10 @@ __device__ __forceinline__ void each_candidate(const Row &row, const uint32_t *m
         }
     }
 }
-// The k largest keys of a row into sh.list, in any order; sh.n: how many there are.  Digit by digit from the top: how many candidates
+// The k largest keys of a row, or of the tiles first, first + of, ... of it, into sh.list, in any order; sh.n: how many there are.  Digit by digit from the top: how many candidates
 // have each value of the digit below the digits settled so far, and in which of them the k-th largest lies.  By all wavefronts.
 template <typename T, bool MASK>
-__device__ __forceinline__ void select_row(TopShared &sh, const Row &row, const uint32_t *mask, int V, int k, int wave, int nw, int lane) {
+__device__ __forceinline__ void select_row(TopShared &sh, const Row &row, const uint32_t *mask, int V, int k, int first, int of, int wave, int nw, int lane) {
     const int tid = wave * WAVE + lane;
     if (tid == 0) {
         sh.prefix = 0;
@@ -650,7 +702,7 @@ __device__ __forceinline__ void select_row(TopShared &sh, const Row &row, const 
         for (int i = tid; i < BINS; i += nw * WAVE) sh.bin[i] = 0;
         __syncthreads();
         const uint64_t prefix = sh.prefix;
-        each_candidate<T, MASK>(row, mask, V, wave, nw, lane, [&](uint64_t key) __attribute__((always_inline)) {
+        each_candidate<T, MASK>(row, mask, V, first, of, lane, [&](uint64_t key) __attribute__((always_inline)) {
             if ((key >> shift) >> DIGIT == prefix) atomicAdd(&sh.bin[(key >> shift) & (BINS - 1)], 1u);
         });
         __syncthreads();
@@ -679,7 +731,7 @@ __device__ __forceinline__ void select_row(TopShared &sh, const Row &row, const 
         if (sh.settled || shift == 0) break;
     }
     const uint64_t least = sh.settled == 2 ? 1ull : sh.prefix << shift;
-    each_candidate<T, MASK>(row, mask, V, wave, nw, lane, [&](uint64_t key) __attribute__((always_inline)) {
+    each_candidate<T, MASK>(row, mask, V, first, of, lane, [&](uint64_t key) __attribute__((always_inline)) {
         if (key >= least) {
             const uint32_t i = atomicAdd(&sh.n, 1u);
             if (i < MOST_LISTED) sh.list[i] = key;   // (k of them, or all there are)
@@ -748,107 +800,171 @@ __device__ __forceinline__ void list_group(TopShared &sh, const u32x4 &raw, uint
         }
     }
 }
-template <typename T, bool MASK, bool W>
+// The row's first k of n listed keys, by all threads: f(place, key) for each of them, in no order.
+template <typename F> __device__ __forceinline__ void each_place(const TopShared &sh, int n, int k, F f) {
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const uint64_t key = sh.list[i];
+        int place = 0;
+        for (int j = 0; j < n; j++) place += sh.list[j] > key;   // how many are larger
+        if (place < k && key) f(place, key);
+    }
+}
+// A split row's candidates lie behind its parts' sums, k to a part, two words each: the logit's order and the token's complement.
+static_assert((sizeof(SplitRow) / sizeof(Marked) - PPV_SPLIT_MAX_PARTS * PART_WORDS) / 2 <= MOST_LISTED, "all parts' candidates are listed together");
+int most_parts(int k) { return ((int)(sizeof(SplitRow) / sizeof(Marked)) - PPV_SPLIT_MAX_PARTS * PART_WORDS) / (2 * k); }
+template <typename T, bool MASK, bool W, bool SPLIT>
 __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restrict__ logits, int64_t row_stride, const int32_t *__restrict__ tokens,
-                                                              const uint32_t *__restrict__ mask, int V, int n_words, int B, int k,
-                                                              int32_t *__restrict__ top_ids, float *__restrict__ top_logprobs, Outputs out, Temper tp) {
+                                                              const uint32_t *__restrict__ mask, int V, int n_words, int k, int shift, SplitScratch *scratch,
+                                                              uint32_t mark, int32_t *__restrict__ top_ids, float *__restrict__ top_logprobs, Outputs out, Temper tp) {
     using G = TileGeom<T>;
     __shared__ TopShared sh;
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = blockDim.x / WAVE;
+    const int64_t b = blockIdx.x >> (SPLIT ? shift : 0);
+    Split sp = split_of<SPLIT>(shift);
+    const int tok = tokens ? tokens[b] : V;
+    int32_t *ids = top_ids + b * k;
+    float *lps = top_logprobs + b * k;
+    if (tok < 0) {   // left out
+        if (sp.part != 0) return;
+        if (threadIdx.x == 0) put_values(out, b, {0.f, 0.f, 0.f});
+        for (int i = threadIdx.x; i < k; i += blockDim.x) {
+            ids[i] = -1;
+            lps[i] = -INFINITY;
+        }
+        return;
+    }
+    const T *at = logits + b * row_stride;
+    const Row row = row_of(at, V);
+    const uint32_t *mrow = MASK ? mask + b * n_words : nullptr;
+    float x = wave == 0 ? logit_of(at, mrow, tok, V) : 0.f;
+    const int first = sp.part * nw + wave, of = sp.parts * nw;
+    const Share share = share_of(tiles_in<T>(V), first, of);
     const float step = RAISE * __builtin_amdgcn_rcpf(tp.c);
+    Tally a = no_tally();
+    Best best = {-INFINITY, -INFINITY, 0};
     {
-        const int64_t b = blockIdx.x;
-        const int tok = tokens ? tokens[b] : V;
-        int32_t *ids = top_ids + b * k;
-        float *lps = top_logprobs + b * k;
-        if (tok < 0) {   // left out
-            if (threadIdx.x == 0) put_values(out, b, {0.f, 0.f, 0.f});
-            for (int i = threadIdx.x; i < k; i += blockDim.x) {
-                ids[i] = -1;
-                lps[i] = -INFINITY;
-            }
-            return;
+        MaskedTile<T, MASK> now, next;
+        now.load(row, mrow, share.n > 0 ? share.at(0) : NO_TILE, lane, V);
+        for (int i = 0; i < share.n; i++) {
+            next.load(row, mrow, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane, V);
+            const int tile = share.at(i), left = tokens_left<T>(V, tile, lane);
+            now.settle(tile, lane, V);
+            if ((tile + 1) * G::TILE <= V) top_tile_as<T, MASK, W, false>(now, i, left, lane, tp.c, step, a, best);
+            else top_tile_as<T, MASK, W, true>(now, i, left, lane, tp.c, step, a, best);
+            now = next;
         }
-        const T *at = logits + b * row_stride;
-        const Row row = row_of(at, V);
-        const uint32_t *mrow = MASK ? mask + b * n_words : nullptr;
-        const float x = wave == 0 ? logit_of(at, mrow, tok, V) : 0.f;
-        const Share share = share_of(tiles_in<T>(V), wave, nw);
-        Tally a = no_tally();
-        Best best = {-INFINITY, -INFINITY, 0};
-        {
-            MaskedTile<T, MASK> now, next;
-            now.load(row, mrow, share.n ? share.at(0) : NO_TILE, lane, V);
-            for (int i = 0; i < share.n; i++) {
-                next.load(row, mrow, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane, V);
-                const int tile = share.at(i), left = tokens_left<T>(V, tile, lane);
-                now.settle(tile, lane, V);
-                if ((tile + 1) * G::TILE <= V) top_tile_as<T, MASK, W, false>(now, i, left, lane, tp.c, step, a, best);
-                else top_tile_as<T, MASK, W, true>(now, i, left, lane, tp.c, step, a, best);
-                now = next;
-            }
+    }
+    const uint32_t mine = best.first == -INFINITY ? 0u : order_of(best.first), other = best.second == -INFINITY ? 0u : order_of(best.second);
+    sh.best[wave * WAVE + lane] = mine;
+    if (nw * 2 <= MOST_WAVES) sh.best[(nw + wave) * WAVE + lane] = other;
+    if (threadIdx.x == 0) sh.n = 0;
+    Part p = workgroup_part<false, W, false>(sh.row, a, x, wave, nw, lane);   // (a barrier behind what is above)
+    if (wave == 0) {
+        if (SPLIT) {
+            find_area<SPLIT>(sp, scratch, (int)b, mark);
+            send_part(sp, p, lane);
         }
-        const uint32_t mine = best.first == -INFINITY ? 0u : order_of(best.first);
-        const uint32_t other = best.second == -INFINITY ? 0u : order_of(best.second);
-        sh.best[wave * WAVE + lane] = mine;
-        if (nw * 2 <= MOST_WAVES) sh.best[(nw + wave) * WAVE + lane] = other;
-        if (threadIdx.x == 0) sh.n = 0;
-        const RowSums r = row_sums<T, MASK, W, false, true>(sh.row, row, mrow, V, a, x, wave, nw, lane, tp.c);   // (a barrier behind what is above)
-        if (threadIdx.x == 0) put_values(out, b, row_values<false>(r.q, r.q, r.x, tp));
-        if (wave == 0) {
-            uint32_t u[MOST_WAVES];
+        uint32_t u[MOST_WAVES];
 #pragma unroll
-            for (int i = 0; i < MOST_WAVES; i++) u[i] = i < (nw * 2 <= MOST_WAVES ? 2 * nw : nw) ? sh.best[i * WAVE + lane] : 0u;
-            uint32_t bound;
-            if (k <= QUARTER) {
-                uint32_t q[MOST_WAVES / 4];
+        for (int i = 0; i < MOST_WAVES; i++) u[i] = i < (nw * 2 <= MOST_WAVES ? 2 * nw : nw) ? sh.best[i * WAVE + lane] : 0u;
+        uint32_t bound;
+        if (k <= QUARTER) {
+            uint32_t q[MOST_WAVES / 4];
 #pragma unroll
-                for (int i = 0; i < MOST_WAVES / 4; i++) q[i] = max(max(u[i], u[i + 4]), max(u[i + 8], u[i + 12]));
-                bound = bound_of(q, k);
-            } else {
-                bound = bound_of(u, k);
-            }
-            if (lane == 0) sh.bound = bound;
-        }
-        __syncthreads();
-        const uint32_t bound = sh.bound;
-        const bool more = other >= bound;
-        auto look = [&](int i, int l) __attribute__((always_inline)) {   // at lane l's group i
-            const int v = share.at(i >> 2) * G::TILE + (i & 3) * G::PER_LOAD + l * G::EPL;
-            list_group<T>(sh, __builtin_amdgcn_raw_buffer_load_b128(row.buf, (uint32_t)v * (uint32_t)sizeof(T), 0, 0),
-                          MASK ? bits_at<T>(mrow, v, V) : 0xFFu, v, V, bound);
-        };
-        if (mine >= bound && !more) look(best.at, lane);
-        // lanes with more than one such group: all of theirs are looked at again, one lane's by the whole wavefront or each its own
-        const uint64_t lanes = __ballot(more);
-        if (__popcll(lanes) * ((share.n * 4 + WAVE - 1) / WAVE) > share.n * 4) {
-            if (more)
-                for (int i = 0; i < share.n * 4; i++) look(i, lane);
+            for (int i = 0; i < MOST_WAVES / 4; i++) q[i] = max(max(u[i], u[i + 4]), max(u[i + 8], u[i + 12]));
+            bound = bound_of(q, k);
         } else {
-            for (uint64_t rest = lanes; rest; rest &= rest - 1ull)
-                for (int i = lane; i < share.n * 4; i += WAVE) look(i, __ffsll((long long)rest) - 1);
+            bound = bound_of(u, k);
+        }
+        if (lane == 0) sh.bound = bound;
+    }
+    __syncthreads();
+    const uint32_t bound = sh.bound;
+    const bool more = other >= bound;
+    auto look = [&](int i, int l) __attribute__((always_inline)) {   // at lane l's group i
+        const int v = share.at(i >> 2) * G::TILE + (i & 3) * G::PER_LOAD + l * G::EPL;
+        list_group<T>(sh, __builtin_amdgcn_raw_buffer_load_b128(row.buf, (uint32_t)v * (uint32_t)sizeof(T), 0, 0),
+                      MASK ? bits_at<T>(mrow, v, V) : 0xFFu, v, V, bound);
+    };
+    if (mine >= bound && !more) look(best.at, lane);
+    // lanes with more than one such group: all of theirs are looked at again, one lane's by the whole wavefront or each its own
+    const uint64_t lanes = __ballot(more);
+    if (__popcll(lanes) * ((share.n * 4 + WAVE - 1) / WAVE) > share.n * 4) {
+        if (more)
+            for (int i = 0; i < share.n * 4; i++) look(i, lane);
+    } else {
+        for (uint64_t rest = lanes; rest; rest &= rest - 1ull)
+            for (int i = lane; i < share.n * 4; i += WAVE) look(i, __ffsll((long long)rest) - 1);
+    }
+    __syncthreads();
+    int n = (int)sh.n;
+    if (n > MOST_LISTED) {   // tokens that are too much alike
+        __syncthreads();
+        select_row<T, MASK>(sh, row, mrow, V, k, first, of, wave, nw, lane);
+        n = (int)sh.n;
+    }
+    if (SPLIT) {
+        find_area<SPLIT>(sp, scratch, (int)b, mark);
+        Marked *words = (Marked *)sp.row + PPV_SPLIT_MAX_PARTS * PART_WORDS;
+        each_place(sh, n, k, [&](int place, uint64_t key) __attribute__((always_inline)) {
+            Marked *w = words + 2 * (sp.part * k + place);
+            send(w, __uint_as_float((uint32_t)(key >> TOKEN_BITS)), sp.mark);
+            send(w + 1, __uint_as_float((uint32_t)key & TOKEN_MASK), sp.mark);
+        });
+        for (int i = n + (int)threadIdx.x; i < k; i += blockDim.x) {   // (the places that no candidate has)
+            send(words + 2 * (sp.part * k + i), 0.f, sp.mark);
+            send(words + 2 * (sp.part * k + i) + 1, 0.f, sp.mark);
+        }
+        __syncthreads();   // the workgroup's words are sent
+        if (wave == 0) {
+            const PartWords w = look_at_parts(sp, lane);
+            int last = 0;
+            if (lane == 0) last = arrive(sp) ? 1 : 0;
+            last = __builtin_amdgcn_readfirstlane(last);
+            if (last) {
+                p = receive_parts<false, W>(sp, w, lane);
+                if (lane == 0) {
+                    sh.row.met = p;
+                    sh.n = 0;
+                }
+            }
+            if (lane == 0) sh.row.mine = last;
         }
         __syncthreads();
-        uint32_t n = sh.n;
+        if (!sh.row.mine) return;
+        p = sh.row.met;
+        const int most = sp.parts * k;
+        for (int i0 = wave * WAVE; i0 < most; i0 += nw * WAVE) {   // (by whole wavefronts)
+            const int i = min(i0 + lane, most - 1);
+            Marked o, t;
+            auto look_again = [&]() __attribute__((always_inline)) {
+                o = shared_get(words + 2 * i);
+                t = shared_get(words + 2 * i + 1);
+            };
+            look_again();
+            const bool come = wait_for(sp, [&]() __attribute__((always_inline)) { return has(o, sp.mark) && has(t, sp.mark); }, look_again);
+            shared_put(words + 2 * i, (Marked)0);
+            shared_put(words + 2 * i + 1, (Marked)0);
+            if (!come && lane == 0) sh.row.mine = NOT_COME;
+            const uint64_t key = come ? (uint64_t)(uint32_t)o << TOKEN_BITS | ((uint32_t)t & TOKEN_MASK) : 0ull;
+            if (i0 + lane < most && key) sh.list[atomicAdd(&sh.n, 1u)] = key;
+        }
         __syncthreads();
-        if (n > MOST_LISTED) {   // tokens that are too much alike
-            select_row<T, MASK>(sh, row, mrow, V, k, wave, nw, lane);
-            n = sh.n;
+        n = (int)sh.n;
+        if (sh.row.mine == NOT_COME) {   // no candidates then, and a sum that is none
+            n = 0;
+            p.all.s = __uint_as_float(0x7FC00000u);
         }
-        for (int i = threadIdx.x; i < k; i += blockDim.x)
-            if (i >= (int)n) {
-                ids[i] = -1;
-                lps[i] = -INFINITY;
-            }
-        for (int i = threadIdx.x; i < (int)n; i += blockDim.x) {   // a candidate's place: how many are larger
-            const uint64_t key = sh.list[i];
-            int place = 0;
-            for (int j = 0; j < (int)n; j++) place += sh.list[j] > key;
-            if (place < k) {
-                ids[place] = (int32_t)(TOKEN_MASK - ((uint32_t)key & TOKEN_MASK));
-                lps[place] = row_values<false>(r.q, r.q, logit_at((uint32_t)(key >> TOKEN_BITS)), tp).logprob;
-            }
-        }
+    }
+    const RowSums r = row_sums<T, MASK, false, true>(sh.row, row, mrow, V, p, wave, nw, lane, tp.c);
+    if (threadIdx.x == 0) put_values(out, b, row_values<false>(r.q, r.q, x, tp));
+    each_place(sh, n, k, [&](int place, uint64_t key) __attribute__((always_inline)) {
+        ids[place] = (int32_t)(TOKEN_MASK - ((uint32_t)key & TOKEN_MASK));
+        lps[place] = row_values<false>(r.q, r.q, logit_at((uint32_t)(key >> TOKEN_BITS)), tp).logprob;
+    });
+    for (int i = n + (int)threadIdx.x; i < k; i += blockDim.x) {
+        ids[i] = -1;
+        lps[i] = -INFINITY;
     }
 }
 
@@ -878,6 +994,25 @@ Shape shape_of(int V, ppv_dtype dt, int B) {
     const int nt = tiles_of(V, dt);
     if (nt == 1) return {SHORT_ROWS * WAVE, SHORT_ROWS, true};
     return {(unsigned)waves_of(nt, B) * WAVE, 1, false};
+}
+// The workgroups of a row (1 << shift), and where they meet.
+struct Area {
+    int shift;
+    SplitScratch *scratch;
+};
+Area area_for(int V, ppv_dtype dt, int B, int most, hipStream_t stream) {
+    const int nt = tiles_of(V, dt);
+    int shift = 0;
+    if (B <= PPV_SPLIT_MAX_ROWS) {
+        if (const int v = ppv_tuning(PPV_TUNE_ROW_SPLIT)) {
+            while ((2 << shift) <= v) shift++;
+        } else {
+            while ((B << (shift + 1)) <= 256 && (1 << (shift + 1)) <= PPV_SPLIT_MAX_PARTS && nt >> (shift + 1) >= 4) shift++;
+        }
+        while (shift && ((1 << shift) > most || 2 << shift > nt)) shift--;   // two tiles each
+    }
+    SplitScratch *scratch = shift ? ppv_split_scratch(stream, B) : nullptr;
+    return {scratch ? shift : 0, scratch};
 }
 template <typename P> P *from_row(P *p, int64_t b, int64_t stride = 1) { return p ? p + b * stride : nullptr; }
 
@@ -945,13 +1080,16 @@ template <typename F> ppv_status in_turns(Rows r, int B, F launch) {
     return PPV_OK;
 }
 
-template <typename T, bool MASK, bool W> void launch_score(const Rows &r, const Shape &sh, const Outputs &out, const Temper &tp) {
-    const unsigned grid = sh.groups(r.n), block = sh.block;
+template <typename T, bool MASK, bool W> void launch_score(const Rows &r, const Shape &sh, const Area &area, const Outputs &out, const Temper &tp) {
+    const unsigned grid = sh.groups(r.n) << area.shift, block = sh.block;
     hipStream_t hs = r.stream;
-    if (sh.one)
-        PPV_LAUNCH((score_kernel<T, MASK, W, true>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, from_row(out, r.at), tp);
-    else
-        PPV_LAUNCH((score_kernel<T, MASK, W, false>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, from_row(out, r.at), tp);
+#define PPV_SCORE(ONE, SPLIT)                                                                                                           \
+    PPV_LAUNCH((score_kernel<T, MASK, W, ONE, SPLIT>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n,    \
+               area.shift, area.scratch, ppv_split_mark(area.shift), from_row(out, r.at), tp)
+    if (sh.one) PPV_SCORE(true, false);
+    else if (area.shift) PPV_SCORE(false, true);
+    else PPV_SCORE(false, false);
+#undef PPV_SCORE
 }
 template <typename T, bool MASK, bool H>
 void launch_gradient(const Rows &r, const Shape &sh, int parts, void *d_logits, int64_t d_stride, const float *stats, const Upstream &up, const Temper &tp) {
@@ -980,11 +1118,15 @@ void launch_score_gradient(const Rows &r, const Shape &sh, int held, void *d_log
 #undef PPV_SCORE_GRADIENT
 }
 template <typename T, bool MASK, bool W>
-void launch_top(const Rows &r, unsigned block, int k, int32_t *top_ids, float *top_logprobs, const Outputs &out, const Temper &tp) {
-    const unsigned grid = (unsigned)r.n;
+void launch_top(const Rows &r, unsigned block, const Area &area, int k, int32_t *top_ids, float *top_logprobs, const Outputs &out, const Temper &tp) {
+    const unsigned grid = (unsigned)r.n << area.shift;
     hipStream_t hs = r.stream;
-    PPV_LAUNCH((top_kernel<T, MASK, W>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, k, top_ids + r.at * k,
-               top_logprobs + r.at * k, from_row(out, r.at), tp);
+#define PPV_TOP(SPLIT)                                                                                                                  \
+    PPV_LAUNCH((top_kernel<T, MASK, W, SPLIT>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, k, area.shift,  \
+               area.scratch, ppv_split_mark(area.shift), top_ids + r.at * k, top_logprobs + r.at * k, from_row(out, r.at), tp)
+    if (area.shift) PPV_TOP(true);
+    else PPV_TOP(false);
+#undef PPV_TOP
 }
 
 }  // namespace
@@ -997,9 +1139,11 @@ extern "C" ppv_status ppv_token_logprobs(const void *logits, ppv_dtype dt, int64
     if (st != PPV_OK || B == 0) return st;
     if ((logprobs && !tokens) || (!logprobs && !logZ_valid && !entropy && !stats) || ((uintptr_t)stats & 15u) != 0) return PPV_EINVAL;
     const Outputs out = {logprobs, logZ_valid, entropy, stats};
-    const Shape sh = shape_of(V, dt, B);
+    Shape sh = shape_of(V, dt, B);
+    const Area area = area_for(V, dt, B, PPV_SPLIT_MAX_PARTS, (hipStream_t)stream);
+    if (area.shift) sh.block = (unsigned)waves_of((tiles_of(V, dt) + (1 << area.shift) - 1) >> area.shift, (int64_t)B << area.shift) * WAVE;
     return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
-#define PPV_CALL(T, MASK, W) launch_score<T, MASK, W>(r, sh, out, tp)
+#define PPV_CALL(T, MASK, W) launch_score<T, MASK, W>(r, sh, area, out, tp)
         PPV_PICK(dt, mask, entropy || stats, PPV_CALL);
 #undef PPV_CALL
     });
@@ -1062,9 +1206,10 @@ extern "C" ppv_status ppv_top_logprobs(const void *logits, ppv_dtype dt, int64_t
     if (st != PPV_OK || B == 0) return st;
     if (!top_ids || !top_logprobs || (logprobs && !tokens)) return PPV_EINVAL;
     const Outputs out = {logprobs, nullptr, entropy, nullptr};
-    const unsigned block = (unsigned)waves_of(tiles_of(V, dt), B) * WAVE;
+    const Area area = area_for(V, dt, B, most_parts(k), (hipStream_t)stream);
+    const unsigned block = (unsigned)waves_of((tiles_of(V, dt) + (1 << area.shift) - 1) >> area.shift, (int64_t)B << area.shift) * WAVE;
     return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
-#define PPV_CALL(T, MASK, W) launch_top<T, MASK, W>(r, block, k, top_ids, top_logprobs, out, tp)
+#define PPV_CALL(T, MASK, W) launch_top<T, MASK, W>(r, block, area, k, top_ids, top_logprobs, out, tp)
         PPV_PICK(dt, mask, entropy, PPV_CALL);
 #undef PPV_CALL
     });

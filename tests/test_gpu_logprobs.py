@@ -7,7 +7,7 @@ import torch
 from paper_2504_09135_amd import binding as ppv
 from paper_2504_09135_amd import workloads as W
 
-from gpu_helpers import DEV, to_dev
+from gpu_helpers import DEV, to_dev, tuning
 from logprobs_oracle import WEIGHT, Scores, bf16, check_gradient, check_values, pack, unpack
 
 pytestmark = pytest.mark.gpu
@@ -169,6 +169,70 @@ def test_temperatures(T, dtype):
     x = rng.normal(0, 3, (B, V))
     valid = hand_made_masks(B, V, rng)
     Case(x, dtype, valid, tokens_for(valid, B, V, rng), T=T).check_all((10,))
+
+
+@pytest.mark.parametrize("waves", [0, 1, 4])
+@pytest.mark.parametrize("split", [1, 2, 4, 16])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_split_rows(dtype, split, waves):
+    """Rows over several workgroups, whatever the library would choose: lengths that leave a part without a tile, all masks, all k."""
+    with tuning(ppv.PPV_TUNE_ROW_SPLIT, split), tuning(ppv.PPV_TUNE_WAVES_PER_ROW, waves):
+        for B, V in ((9, 4100), (3, 33000), (17, 50265), (9, 200003)):
+            rng = np.random.default_rng(V + split)
+            x = rng.normal(0, 2.5, (B, V))
+            valid = hand_made_masks(B, V, rng)
+            Case(x, dtype, valid, tokens_for(valid, B, V, rng), T=0.8).check_all((1, 20, 64, 128))
+            Case(x, dtype, None, tokens_for(None, B, V, rng)).check_all((5,))
+        for kind in ("ties", "filtered", "late peak", "lowest"):
+            x = odd_values(kind, 8, 40000, rng)
+            valid = hand_made_masks(8, 40000, rng)
+            Case(x, dtype, valid, tokens_for(valid, 8, 40000, rng)).check_all((3, 100))
+
+
+def test_one_area_for_calls_of_every_kind():
+    """The calls that split rows share a stream's scratch area, one after the other, and leave nothing in it that another takes for its own;
+    graphs that hold them are replayed beside eager calls."""
+    rng = np.random.default_rng(6)
+    B, V = 6, 128256
+    valid = hand_made_masks(B, V, rng)
+    c = Case(rng.normal(0, 2, (B, V)), "bf16", valid, tokens_for(valid, B, V, rng))
+    u = to_dev(rng.random(B, dtype=np.float32))
+    f = lambda *s, **kw: torch.zeros(s, device=DEV, **kw)  # noqa: E731
+    outs = [f(B, dtype=torch.int32), f(B), f(B), f(B), f(B), f(B, 9, dtype=torch.int32), f(B, 9), f(B)]
+
+    def calls():
+        ids, lzv, lp, lz, h, top, tops, mine = outs
+        ppv.constrained_sample(c.logits, c.mask, u, ids, lzv)
+        ppv.ppv_token_logprobs(c.logits, c.tokens, lp, mask=c.mask, logZ_valid=lz, entropy=h)
+        ppv.ppv_top_logprobs(c.logits, 9, top, tops, mask=c.mask, tokens=c.tokens, logprobs=mine)
+
+    with tuning(ppv.PPV_TUNE_ROW_SPLIT, 1):
+        calls()
+        torch.cuda.synchronize()
+        alone = [t.clone() for t in outs]
+    for split in (0, 4, 16, 2):
+        with tuning(ppv.PPV_TUNE_ROW_SPLIT, split):
+            for _ in range(3):
+                for t in outs:
+                    t.fill_(7)
+                calls()
+            graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+            torch.cuda.synchronize()
+            for g in graphs:
+                with torch.cuda.graph(g):
+                    calls()
+        first = None
+        for i in range(4):
+            for t in outs:
+                t.fill_(7)
+            torch.cuda.synchronize()
+            graphs[i % 2].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(outs[0], alone[0]) and torch.equal(outs[5], alone[5])
+            check_values(outs[2].cpu().numpy(), c.ref.logprobs, "logprobs")
+            check_values(outs[6].cpu().numpy(), c.ref.top(9)[1], "top_logprobs")
+            first = first or [t.clone() for t in outs]
+            assert all(torch.equal(a, b) for a, b in zip(outs, first))      # the same to the bit, whatever arrived last
 
 
 def odd_values(kind, B, V, rng):
