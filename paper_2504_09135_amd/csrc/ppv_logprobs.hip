@@ -96,7 +96,23 @@ template <int N, bool W> __device__ __forceinline__ void add(Run &a, const float
         if (W) a.w = fmaf(most(y, FAINT), e, a.w);   // (-inf: nothing, not a NaN)
     }
 }
-__device__ __forceinline__ float if_bit(float x, uint32_t bits, int k) { return (bits >> k) & 1u ? x : -INFINITY; }
+__device__ __forceinline__ uint32_t all_ones_if(uint32_t bits, int k) { return (uint32_t)__builtin_amdgcn_sbfe((int)bits, (uint32_t)k, 1u); }
+__device__ __forceinline__ float if_bit(float x, uint32_t bits, int k) {
+    const uint32_t m = all_ones_if(bits, k);
+    return __uint_as_float((m & __float_as_uint(x)) | (~m & 0xFF800000u));   // x or -inf
+}
+// Valid tokens with a reference of their own
+template <int N, bool W> __device__ __forceinline__ void take_few(Tally &a, const float (&x)[N], float c, float step) {
+    a.few_top = N == 1 ? most(a.few_top, x[0]) : most_of<N>(x, a.few_top);
+    const bool up = a.few_top > a.few_limit;
+    if (__ballot(up) != 0ull) {
+        const float r = up ? reference_at(a.few_top, c) : a.few.r;
+        refer(a.few.s, a.few.w, a.few.r - r);
+        a.few.r = r;
+        a.few_limit = up ? a.few_top + step : a.few_limit;
+    }
+    add<N, W>(a.few, x, c);
+}
 // A group of a lane's tokens, `bits`: the valid ones.  Where few lanes have any, those are summed by themselves; else with the exponentials
 // that are there, unless a lane's weigh too little against its reference for that.
 constexpr int FEW_LANES = 12;
@@ -116,7 +132,7 @@ template <int N, bool MASK, bool W> __device__ __forceinline__ void take_group(T
         for (int i = 0; i < N; i++) {
             const float y = fmaf(x[i], c, -a.all.r), e = fast_exp2(y);
             a.all.s += e;
-            const float v = __uint_as_float(__float_as_uint(e) & (uint32_t)((int32_t)(bits << (31 - i)) >> 31));
+            const float v = __uint_as_float(__float_as_uint(e) & all_ones_if(bits, i));
             s += v;
             if (W) w = fmaf(most(y, FAINT), v, w);
         }
@@ -128,15 +144,7 @@ template <int N, bool MASK, bool W> __device__ __forceinline__ void take_group(T
         const uint32_t mine = alone ? bits : 0u;
 #pragma unroll
         for (int i = 0; i < N; i++) x[i] = if_bit(x[i], mine, i);
-        a.few_top = most_of<N>(x, a.few_top);
-        const bool up = a.few_top > a.few_limit;
-        if (__ballot(up) != 0ull) {
-            const float r = up ? reference_at(a.few_top, c) : a.few.r;
-            refer(a.few.s, a.few.w, a.few.r - r);
-            a.few.r = r;
-            a.few_limit = up ? a.few_top + step : a.few_limit;
-        }
-        add<N, W>(a.few, x, c);
+        take_few<N, W>(a, x, c, step);
     }
 }
 
@@ -183,23 +191,62 @@ template <typename T, bool PAD> __device__ __forceinline__ void unpack_group(con
         for (int k = 0; k < Elem<T>::EPL; k++) x[k] = k < left ? x[k] : -INFINITY;
     }
 }
-template <typename T, bool MASK, bool W, bool PAD>
-__device__ __forceinline__ void take_tile_as(const MaskedTile<T, MASK> &mt, int left, int lane, float c, float step, Tally &a) {
+// A tile with at most two valid tokens in each word of its mask, which is what an ordinary prefix has: those are asked for once more by
+// themselves (from cache; they come while the tile is summed), a word's to a lane, and cost an exponential or two in all.
+template <typename T> struct Gathered {
+    float x[2];
+    __device__ __forceinline__ void load(const Row &row, uint32_t w, int tile, int lane) {
+        const uint32_t at = (uint32_t)tile * (TileGeom<T>::TILE * sizeof(T)) + (uint32_t)lane * (32 * sizeof(T)), w2 = w & (w - 1u);
+        x[0] = load_at(row, w ? at + (uint32_t)__builtin_ctz(w) * (uint32_t)sizeof(T) : OUTSIDE);
+        x[1] = load_at(row, w2 ? at + (uint32_t)__builtin_ctz(w2) * (uint32_t)sizeof(T) : OUTSIDE);
+    }
+    static constexpr uint32_t OUTSIDE = 0xFFFFFF00u;   // behind every row: nothing is read
+    __device__ static __forceinline__ float load_at(const Row &row, uint32_t at) {
+        if (sizeof(T) == 4) return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(row.buf, at, 0, 0));
+        return __uint_as_float((uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(row.buf, at, 0, 0) << 16);
+    }
+};
+template <typename T, bool MASK, bool W, bool PAD, bool FEW>
+__device__ __forceinline__ void take_groups(const MaskedTile<T, MASK> &mt, int left, int lane, float c, float step, Tally &a) {
 #pragma unroll
     for (int j = 0; j < 4; j++) {
         float x[Elem<T>::EPL];
         unpack_group<T, PAD>(mt.t.r[j], left - j * TileGeom<T>::PER_LOAD, x);
-        const uint32_t bits = mt.valid(j, lane);
-        if (MASK) a.seen |= bits;
-        take_group<Elem<T>::EPL, MASK, W>(a, x, bits, c, step);
+        if (FEW) {
+            a.top = most_of<Elem<T>::EPL>(x, a.top);
+            raise<true>(a, c, step);
+            add<Elem<T>::EPL, false>(a.all, x, c);
+        } else {
+            take_group<Elem<T>::EPL, MASK, W>(a, x, mt.valid(j, lane), c, step);
+        }
         __builtin_amdgcn_sched_barrier(0);   // one group's tokens in registers at a time
     }
 }
 template <typename T, bool MASK, bool W>
-__device__ __forceinline__ void take_tile(const MaskedTile<T, MASK> &mt, int tile, int V, int lane, float c, float step, Tally &a) {
+__device__ __forceinline__ void take_tile(const Row &row, const MaskedTile<T, MASK> &mt, int tile, int V, int lane, float c, float step, Tally &a) {
     const int left = tokens_left<T>(V, tile, lane);
-    if ((tile + 1) * TileGeom<T>::TILE <= V) take_tile_as<T, MASK, W, false>(mt, left, lane, c, step, a);
-    else take_tile_as<T, MASK, W, true>(mt, left, lane, c, step, a);
+    const bool whole = (tile + 1) * TileGeom<T>::TILE <= V;
+    if (MASK) {
+        const uint32_t w = mt.t.word, w2 = w & (w - 1u);
+        a.seen |= w & ~LOST ? 1u : w >> 31;
+        if (__ballot((w2 & (w2 - 1u)) != 0u) == 0ull) {
+            Gathered<T> g;
+            g.load(row, w, tile, lane);
+            if (whole) take_groups<T, MASK, W, false, true>(mt, left, lane, c, step, a);
+            else take_groups<T, MASK, W, true, true>(mt, left, lane, c, step, a);
+            if (__ballot(w != 0u) != 0ull) {
+                const float x0[1] = {w ? g.x[0] : -INFINITY};
+                take_few<1, W>(a, x0, c, step);
+                if (__ballot(w2 != 0u) != 0ull) {
+                    const float x1[1] = {w2 ? g.x[1] : -INFINITY};
+                    take_few<1, W>(a, x1, c, step);
+                }
+            }
+            return;
+        }
+    }
+    if (whole) take_groups<T, MASK, W, false, false>(mt, left, lane, c, step, a);
+    else take_groups<T, MASK, W, true, false>(mt, left, lane, c, step, a);
 }
 // The wavefront's tiles from its i-th on: the next one is on its way while one is summed.
 template <typename T, bool MASK, bool W>
@@ -210,7 +257,7 @@ __device__ __forceinline__ void take_tiles(const Row &row, const uint32_t *mask,
     for (; i < share.n; i++) {
         next.load(row, mask, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane, V);
         now.settle(share.at(i), lane, V);
-        take_tile<T, MASK, W>(now, share.at(i), V, lane, c, step, a);
+        take_tile<T, MASK, W>(row, now, share.at(i), V, lane, c, step, a);
         now = next;
     }
 }
@@ -515,7 +562,7 @@ __device__ __forceinline__ void put_tile_as(T *out, const MaskedTile<T, MASK> &m
             for (int k = 0; k < G::EPL; k++) {
                 const float y = exponent<FAR>(x[k], s.rq, c), e = fast_exp2(y);
                 d[k] = e * (H ? fmaf(s.b, most(y, FAINT), s.a) : s.a);
-                if (MASK) d[k] = (bits >> k) & 1u ? d[k] : 0.f;
+                if (MASK) d[k] = __uint_as_float(__float_as_uint(d[k]) & all_ones_if(bits, k));
             }
         } else {
 #pragma unroll
@@ -617,7 +664,7 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
     for (int i = 0; i < HELD; i++)
         if (i < share.n) {
             held[i].settle(share.at(i), lane, V);
-            take_tile<T, MASK, W>(held[i], share.at(i), V, lane, tp.c, step, a);
+            take_tile<T, MASK, W>(row, held[i], share.at(i), V, lane, tp.c, step, a);
         }
     if (HELD == 0) take_tiles<T, MASK, W>(row, mrow, V, share, 0, lane, tp.c, step, a);
     const Part p = workgroup_part<MASK, W, ONE>(sh, a, x, wave, nw, lane);
