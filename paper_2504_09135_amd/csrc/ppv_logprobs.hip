@@ -8,6 +8,7 @@
 //   d_l            = d_logprob (1[v = t] - q) + d_logZ (q - p) - d_entropy q (log q + entropy),   d_logits = d_l / T
 // A row is read once, by all lanes of its wavefronts, each with its own running reference and sums relative to it; the lanes' sums are
 // brought to one reference at the end.  Sums are fp32: a lane adds at most 4,096 terms of one sign.
+#include <cstdlib>
 #include "ppv_rows.h"
 #include "ppv_split.h"
 
@@ -408,21 +409,32 @@ template <typename T> __device__ __forceinline__ float logit_of(const T *row, co
 
 struct Outputs {
     float *logprobs, *logZ_valid, *entropy, *stats;
+    Marked *words;   // the statistics for the library's own next launch, in the rows' scratch (see STATS_AT)
 };
 struct RowValues {
     float logprob, logZ, entropy;
 };
 // what the sums say.  Without mass (no valid token, or all at -inf): -inf, and an entropy of 0.
-template <bool MASK> __device__ __forceinline__ RowValues row_values(const Sums &all, const Sums &q, float x, const Temper &tp) {
+template <bool MASK> __device__ __forceinline__ RowValues row_values(const Sums &all, const Sums &q, float x, const Temper &tp, float log_s) {
     if (!(q.s != 0.f)) return {-INFINITY, -INFINITY, 0.f};
-    const float log_s = logf(q.s);
     return {(x - q.m) * tp.inv - log_s, MASK ? fmaf(q.m - all.m, tp.inv, log_s - logf(all.s)) : 0.f,
             fmaxf(fmaf(q.w / q.s, -LN2F, log_s), 0.f)};
+}
+template <bool MASK> __device__ __forceinline__ RowValues row_values(const Sums &all, const Sums &q, float x, const Temper &tp) {
+    return row_values<MASK>(all, q, x, tp, logf(q.s));
 }
 __device__ __forceinline__ void put_stats(float *stats, int64_t b, const Sums &all, const Sums &q, const RowValues &v) {
     float4 *at = (float4 *)(stats + b * PPV_LOGPROB_STATS);
     at[0] = {all.m, all.s, q.m, q.s};
     at[1] = {v.entropy, v.logprob, 0.f, 0.f};
+}
+// The words of a row's scratch that hold its statistics between two launches of one call, behind those of the parts: with the call's mark, so
+// that no later call takes one for a word of its own.
+constexpr int STATS_AT = PPV_SPLIT_MAX_PARTS * PART_WORDS, ROW_WORDS = (int)(sizeof(SplitRow) / sizeof(Marked));
+__device__ __forceinline__ void put_words(Marked *words, int64_t b, const Sums &all, const Sums &q, const RowValues &v, uint32_t mark) {
+    const float w[6] = {all.m, all.s, q.m, q.s, v.entropy, v.logprob};
+#pragma unroll
+    for (int i = 0; i < 6; i++) send(words + b * ROW_WORDS + STATS_AT + i, w[i], mark);
 }
 __device__ __forceinline__ void put_values(const Outputs &o, int64_t b, const RowValues &v) {
     if (o.logprobs) o.logprobs[b] = v.logprob;
@@ -480,6 +492,7 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
         const RowValues v = row_values<MASK>(r.all, r.q, x, tp);
         put_values(out, b, v);
         if (out.stats) put_stats(out.stats, b, r.all, r.q, v);
+        if (SPLIT && out.words) put_words(out.words, b, r.all, r.q, v, mark);
     }
 }
 
@@ -488,12 +501,16 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
 struct Upstream {
     const float *logprobs, *logZ_valid, *entropy;
 };
-// d_logits = e_q (a + b y_q) - z e_p, and `at_token` more at the row's token.  y_q = x c - rq, e_q = 2^y_q, e_p = 2^(x c - rp); in rows
-// beyond FAR_OFF y_q = (x - rq) c and e_p likewise.
+// d_logits = e (a + b y) for valid tokens, less e_p z for all of them (a mask, and a slope of log Z), and `at_token` more at the row's token:
+//   TOGETHER   y = x c - r, e = e_p = 2^y with r the reference of all tokens: one exponential a token.  For rows whose valid tokens weigh
+//              2^-TOGETHER_MOST or more of all
+//   else       y and e relative to the valid tokens' reference r, e_p = 2^(x c - rp)
+// In rows beyond FAR_OFF, r and rp are logits, and y = (x - r) c.
+constexpr float TOGETHER_MOST = 24.f;
 struct Slope {
-    float rq, a, b, rp, z, at_token;
+    float r, a, b, rp, z, at_token;
     bool nothing;   // zeros all over the row
-    bool far;
+    bool far, together;
 };
 template <bool MASK> __device__ __forceinline__ Slope slope_of(const Sums &all, const Sums &q, float entropy, float logprob, const Upstream &up, int64_t b, int tok, const Temper &tp) {
     Slope s;
@@ -505,18 +522,27 @@ template <bool MASK> __device__ __forceinline__ Slope slope_of(const Sums &all, 
     s.a = over * (z - g - h * (entropy - logf(q.s)));
     s.b = over * (-LN2F * h);
     s.z = MASK && z != 0.f ? z * tp.inv / all.s : 0.f;
-    s.rq = q.m;
+    s.r = q.m;
     s.rp = all.m;
+    s.together = false;
     if (!s.far) {   // relative to m c as it is rounded
-        s.rq = q.m * c;
+        s.r = q.m * c;
         s.rp = all.m * c;
-        const float dq = fmaf(-q.m, c, s.rq), fq = fast_exp2(dq);
-        s.a = fq * fmaf(s.b, dq, s.a);
-        s.b *= fq;
-        s.z *= fast_exp2(fmaf(-all.m, c, s.rp));
+        float d = fmaf(-q.m, c, s.r);
+        if (MASK) {
+            s.together = __builtin_amdgcn_readfirstlane(s.z != 0.f && s.rp - s.r <= TOGETHER_MOST);
+            if (s.together) {
+                d += s.rp - s.r;
+                s.r = s.rp;
+            }
+            s.z *= fast_exp2(fmaf(-all.m, c, s.rp));
+        }
+        const float f = fast_exp2(d);
+        s.a = f * fmaf(s.b, d, s.a);
+        s.b *= f;
     }
     s.at_token = g * tp.inv;
-    s.rq = uniform(s.rq), s.a = uniform(s.a), s.b = uniform(s.b), s.rp = uniform(s.rp), s.z = uniform(s.z), s.at_token = uniform(s.at_token);
+    s.r = uniform(s.r), s.a = uniform(s.a), s.b = uniform(s.b), s.rp = uniform(s.rp), s.z = uniform(s.z), s.at_token = uniform(s.at_token);
     return s;
 }
 // Values of this lane's tokens from token v on, rounded to the nearest of their type, once.  What lies behind the row is left as it is.
@@ -557,20 +583,33 @@ __device__ __forceinline__ void put_tile_as(T *out, const MaskedTile<T, MASK> &m
         float x[G::EPL], d[G::EPL];
         unpack_fresh<T>(mt.t.r[j], x);
         const uint32_t bits = mt.valid(j, lane);
-        if (!MASK || __ballot(bits != 0u) != 0ull) {
+        const bool any = !MASK || __ballot(bits != 0u) != 0ull;
+        if (MASK && !FAR && s.together) {
+            if (any) {
 #pragma unroll
-            for (int k = 0; k < G::EPL; k++) {
-                const float y = exponent<FAR>(x[k], s.rq, c), e = fast_exp2(y);
-                d[k] = e * (H ? fmaf(s.b, most(y, FAINT), s.a) : s.a);
-                if (MASK) d[k] = __uint_as_float(__float_as_uint(d[k]) & all_ones_if(bits, k));
+                for (int k = 0; k < G::EPL; k++) {
+                    const float y = fmaf(x[k], c, -s.r), e = fast_exp2(y), t = H ? fmaf(s.b, most(y, FAINT), s.a) : s.a;
+                    d[k] = e * (__uint_as_float(__float_as_uint(t) & all_ones_if(bits, k)) - s.z);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < G::EPL; k++) d[k] = -s.z * fast_exp2(fmaf(x[k], c, -s.r));
             }
         } else {
 #pragma unroll
             for (int k = 0; k < G::EPL; k++) d[k] = 0.f;
-        }
-        if (MASK && s.z != 0.f) {
+            if (any) {
 #pragma unroll
-            for (int k = 0; k < G::EPL; k++) d[k] = fmaf(-s.z, fast_exp2(exponent<FAR>(x[k], s.rp, c)), d[k]);
+                for (int k = 0; k < G::EPL; k++) {
+                    const float y = exponent<FAR>(x[k], s.r, c), e = fast_exp2(y);
+                    d[k] = e * (H ? fmaf(s.b, most(y, FAINT), s.a) : s.a);
+                    if (MASK) d[k] = __uint_as_float(__float_as_uint(d[k]) & all_ones_if(bits, k));
+                }
+            }
+            if (MASK && s.z != 0.f) {
+#pragma unroll
+                for (int k = 0; k < G::EPL; k++) d[k] = fmaf(-s.z, fast_exp2(exponent<FAR>(x[k], s.rp, c)), d[k]);
+            }
         }
         const int mine = tok - v;   // the row's token, counted from this lane's first one
         if (__ballot((uint32_t)mine < (uint32_t)G::EPL) != 0ull) {
@@ -611,7 +650,7 @@ template <typename T, bool MASK, bool H, bool ONE>
 __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void gradient_kernel(const T *logits, int64_t row_stride, const int32_t *__restrict__ tokens,
                                                                                             const uint32_t *__restrict__ mask, int V, int n_words, int B, int parts,
                                                                                             T *d_logits, int64_t d_row_stride, const float *__restrict__ stats,
-                                                                                            Upstream up, Temper tp) {
+                                                                                            int stats_stride, int stats_step, Upstream up, Temper tp) {
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = blockDim.x / WAVE;
     const int64_t units = ONE ? B : (int64_t)B * parts;
     const int per = ONE ? SHORT_ROWS : 1;
@@ -620,9 +659,9 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void gra
         const int64_t b = ONE ? u : u / parts;
         const int part = ONE ? 0 : (int)(u - b * parts);
         const int tok = tokens ? tokens[b] : V;
-        const float *st = stats + b * PPV_LOGPROB_STATS;
-        const Sums all = {st[0], st[1], 0.f}, q = {st[2], st[3], 0.f};
-        const Slope s = slope_of<MASK>(all, q, st[4], st[5], up, b, tok, tp);
+        const float *st = stats + b * stats_stride;   // (in the rows' scratch a word is a float and a mark)
+        const Sums all = {st[0], st[stats_step], 0.f}, q = {st[2 * stats_step], st[3 * stats_step], 0.f};
+        const Slope s = slope_of<MASK>(all, q, st[4 * stats_step], st[5 * stats_step], up, b, tok, tp);
         T *to = d_logits + b * d_row_stride;
         const int first = ONE ? 0 : part * nw + wave, of = ONE ? 1 : nw * parts;
         if (s.nothing) {
@@ -634,20 +673,22 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void gra
     }
 }
 
-// Both: the sums, then the gradient.  A wavefront holds its tiles, at most HELD; HELD = 0: they are read again.
+// Both: the sums, then the gradient.  A wavefront holds its tiles, at most HELD; HELD = 0: they are read again.  1 << shift workgroups may
+// have a row: each takes all of its sums, which needs no word from another, and its part of the gradient.
 template <typename T, bool MASK, bool W, bool ONE, int HELD>
 __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void score_gradient_kernel(const T *logits, int64_t row_stride, const int32_t *__restrict__ tokens,
-                                                                                                  const uint32_t *__restrict__ mask, int V, int n_words, int B,
+                                                                                                  const uint32_t *__restrict__ mask, int V, int n_words, int B, int shift,
                                                                                                   T *d_logits, int64_t d_row_stride, Outputs out, Upstream up, Temper tp) {
     __shared__ RowShared sh;
     const int lane = threadIdx.x & (WAVE - 1), wave = ONE ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = ONE ? 1 : blockDim.x / WAVE;
-    const int64_t b = ONE ? (int64_t)blockIdx.x * SHORT_ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) : blockIdx.x;
+    const int64_t b = ONE ? (int64_t)blockIdx.x * SHORT_ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) : blockIdx.x >> shift;
     if (ONE && b >= B) return;
+    const int part = ONE ? 0 : blockIdx.x & ((1 << shift) - 1);
     const int tok = tokens ? tokens[b] : V;
     T *to = d_logits + b * d_row_stride;
     if (tok < 0) {   // left out
-        if (lane == 0 && wave == 0) put_values(out, b, {0.f, 0.f, 0.f});
-        put_zeros(to, wave, nw, lane, V);
+        if (lane == 0 && wave == 0 && part == 0) put_values(out, b, {0.f, 0.f, 0.f});
+        put_zeros(to, part * nw + wave, ONE ? 1 : nw << shift, lane, V);
         return;
     }
     const T *at = logits + b * row_stride;
@@ -670,15 +711,15 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
     const Part p = workgroup_part<MASK, W, ONE>(sh, a, x, wave, nw, lane);
     const RowSums r = row_sums<T, MASK, ONE>(sh, row, mrow, V, p, wave, nw, lane, tp.c);
     const RowValues v = row_values<MASK>(r.all, r.q, x, tp);
-    if (lane == 0 && wave == 0) put_values(out, b, v);
+    if (lane == 0 && wave == 0 && part == 0) put_values(out, b, v);
     const Slope s = slope_of<MASK>(r.all, r.q, v.entropy, v.logprob, up, b, tok, tp);
     if (s.nothing) {
-        put_zeros(to, wave, nw, lane, V);
+        put_zeros(to, part * nw + wave, ONE ? 1 : nw << shift, lane, V);
         return;
     }
 #pragma unroll
-    for (int i = 0; i < HELD; i++)
-        if (i < share.n) put_tile<T, MASK, W>(to, held[i], s, share.at(i), lane, tok, V, tp.c);
+    for (int i = 0; i < HELD; i++)   // (four neighbouring wavefronts' tiles are one part's: those of the four SIMDs)
+        if (i < share.n && (ONE || ((share.at(i) >> 2) & ((1 << shift) - 1)) == part)) put_tile<T, MASK, W>(to, held[i], s, share.at(i), lane, tok, V, tp.c);
     if (HELD == 0) put_tiles<T, MASK, W>(to, row, mrow, s, tok, V, share, 0, lane, tp.c);
 }
 
@@ -703,7 +744,7 @@ constexpr int MOST_LISTED = 1024;   // candidates not below the bound that are s
 struct TopShared {
     RowShared row;
     union {
-        uint32_t best[MOST_WAVES * WAVE];   // each lane's largest token, and (up to eight wavefronts) the largest of its other groups
+        uint32_t best[MOST_WAVES * WAVE];   // each lane's largest token, and (up to two wavefronts) the largest of its other groups
         uint32_t bin[BINS];
     };
     uint64_t list[MOST_LISTED];
@@ -792,8 +833,10 @@ __device__ __forceinline__ void select_row(TopShared &sh, const Row &row, const 
 struct Best {
     float first, second;
     int at;   // 4 i + j: load j of the wavefront's i-th tile
+    float third;   // HELD: the second largest group's place too, and the largest token of the others
+    int at2;
 };
-template <typename T, bool MASK, bool W, bool PAD>
+template <typename T, bool MASK, bool W, bool PAD, bool HELD>
 __device__ __forceinline__ void top_tile_as(const MaskedTile<T, MASK> &mt, int i, int left, int lane, float c, float step, Tally &a, Best &best) {
     constexpr int EPL = Elem<T>::EPL;
 #pragma unroll
@@ -810,20 +853,36 @@ __device__ __forceinline__ void top_tile_as(const MaskedTile<T, MASK> &mt, int i
         a.top = most(a.top, g);
         raise<false>(a, c, step);
         add<EPL, W>(a.all, x, c);
+        if (HELD) {
+            best.third = __builtin_amdgcn_fmed3f(best.second, best.third, g);
+            best.at2 = g > best.first ? best.at : (g > best.second ? 4 * i + j : best.at2);
+        }
         best.second = __builtin_amdgcn_fmed3f(best.first, best.second, g);   // (second <= first)
         best.at = g > best.first ? 4 * i + j : best.at;
         best.first = most(best.first, g);
         __builtin_amdgcn_sched_barrier(0);   // one group's tokens in registers at a time
     }
 }
-// The k-th largest of the lanes' largest tokens, or a little less: at least k tokens are not below it.  1 where fewer lanes have any.  By
-// one wavefront, bit by bit from the top.  Up to QUARTER candidates the lanes' tokens are taken four at a time, which costs a bound that a few
-// more tokens reach and a quarter of the comparisons.
-constexpr int QUARTER = 64, BOUND_BITS = 16;
+// A bound that at least k of the lanes' tokens `u` are not below: the k-th largest of them, or a little less.  1 where there are fewer.  By one
+// wavefront, bit by bit from the first in which they differ.
+constexpr int BOUND_BITS = 12;
+constexpr int FEW_ASKED = 20;   // up to so many candidates the bound is found from 64 tokens: a quarter more tokens reach it
 template <int N> __device__ __forceinline__ uint32_t bound_of(const uint32_t (&u)[N], int k) {
-    uint32_t t = 0u;
-#pragma unroll 1
-    for (int bit = 31; bit >= 32 - BOUND_BITS; bit--) {
+    uint32_t hi = 0u, lo = 0u;   // the largest, and the complement of the smallest that is one
+    int some = 0;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        hi = max(hi, u[i]);
+        lo = max(lo, u[i] ? ~u[i] : 0u);
+        some += __popcll(__ballot(u[i] != 0u));
+    }
+    if (some < k) return 1u;
+    hi = wave_max(hi);
+    lo = ~wave_max(lo);
+    if (hi == lo) return hi;
+    const int first = 31 - __builtin_clz(hi ^ lo);
+    uint32_t t = hi & ~((2u << first) - 1u);
+    for (int bit = first; bit >= 0 && bit > first - BOUND_BITS; bit--) {
         const uint32_t try_at = t | 1u << bit;
         int n = 0;
 #pragma unroll
@@ -833,33 +892,54 @@ template <int N> __device__ __forceinline__ uint32_t bound_of(const uint32_t (&u
     }
     return t > 1u ? t : 1u;
 }
+// the bound as a logit: what is not below it is listed.  (1, no bound: anything but -inf)
+__device__ __forceinline__ float bound_logit(uint32_t bound) { return bound > 1u ? most(logit_at(bound), LOWEST) : LOWEST; }
+// The valid tokens of a group that are not below the bound
 template <typename T>
-__device__ __forceinline__ void list_group(TopShared &sh, const u32x4 &raw, uint32_t bits, int v, int V, uint32_t bound) {
+__device__ __forceinline__ void list_group(TopShared &sh, const u32x4 &raw, uint32_t bits, int v, int V, float bound) {
     constexpr int EPL = Elem<T>::EPL;
     float x[EPL];
+    uint32_t m = 0u;
     unpack_group<T, true>(raw, V - v, x);
 #pragma unroll
-    for (int k = 0; k < EPL; k++) {
-        const uint64_t key = (bits >> k) & 1u ? key_of(x[k], v + k) : 0ull;
-        if (key >> TOKEN_BITS >= bound) {
-            const uint32_t i = atomicAdd(&sh.n, 1u);
-            if (i < MOST_LISTED) sh.list[i] = key;
-        }
+    for (int k = 0; k < EPL; k++) m |= x[k] >= bound ? 1u << k : 0u;
+    m &= bits;
+    if (m) {
+        uint32_t i = atomicAdd(&sh.n, (uint32_t)__builtin_popcount(m));
+        do {   // (one, nearly always)
+            const int k = __builtin_ctz(m);
+            float at = x[0];
+#pragma unroll
+            for (int j = 1; j < EPL; j++) at = k == j ? x[j] : at;
+            if (i < MOST_LISTED) sh.list[i] = key_of(at, v + k);
+            i++;
+            m &= m - 1u;
+        } while (m);
     }
 }
-// The row's first k of n listed keys, by all threads: f(place, key) for each of them, in no order.
-template <typename F> __device__ __forceinline__ void each_place(const TopShared &sh, int n, int k, F f) {
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const uint64_t key = sh.list[i];
+// The row's first k of n listed keys, by all wavefronts: f(place, key) for each of them, in no order.  A key's place is how many are larger:
+// a wavefront has every nw-th key, one to a lane, and counts for one after the other in as many comparisons as there are 64 keys.
+template <typename F> __device__ __forceinline__ void each_place(const TopShared &sh, int n, int k, int wave, int nw, int lane, F f) {
+    for (int i0 = wave; i0 < n; i0 += nw * WAVE) {
+        const int i = i0 + lane * nw, mine = min((n - i0 + nw - 1) / nw, WAVE);
+        const uint64_t key = i < n ? sh.list[i] : 0ull;
         int place = 0;
-        for (int j = 0; j < n; j++) place += sh.list[j] > key;   // how many are larger
+        for (int j0 = 0; j0 < n; j0 += WAVE) {
+            const uint64_t other = j0 + lane < n ? sh.list[j0 + lane] : 0ull;
+            for (int l = 0; l < mine; l++) {
+                const uint64_t it = (uint64_t)lane_value((uint32_t)(key >> 32), l) << 32 | lane_value((uint32_t)key, l);
+                const int larger = __popcll(__ballot(other > it));
+                place += lane == l ? larger : 0;
+            }
+        }
         if (place < k && key) f(place, key);
     }
 }
 // A split row's candidates lie behind its parts' sums, k to a part, two words each: the logit's order and the token's complement.
 static_assert((sizeof(SplitRow) / sizeof(Marked) - PPV_SPLIT_MAX_PARTS * PART_WORDS) / 2 <= MOST_LISTED, "all parts' candidates are listed together");
 int most_parts(int k) { return ((int)(sizeof(SplitRow) / sizeof(Marked)) - PPV_SPLIT_MAX_PARTS * PART_WORDS) / (2 * k); }
-template <typename T, bool MASK, bool W, bool SPLIT>
+// HELD: a wavefront has as many tiles at most, and keeps them in registers.
+template <typename T, bool MASK, bool W, bool SPLIT, int HELD>
 __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restrict__ logits, int64_t row_stride, const int32_t *__restrict__ tokens,
                                                               const uint32_t *__restrict__ mask, int V, int n_words, int k, int shift, SplitScratch *scratch,
                                                               uint32_t mark, int32_t *__restrict__ top_ids, float *__restrict__ top_logprobs, Outputs out, Temper tp) {
@@ -888,22 +968,33 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
     const Share share = share_of(tiles_in<T>(V), first, of);
     const float step = RAISE * __builtin_amdgcn_rcpf(tp.c);
     Tally a = no_tally();
-    Best best = {-INFINITY, -INFINITY, 0};
-    {
+    Best best = {-INFINITY, -INFINITY, 0, -INFINITY, 0};
+    MaskedTile<T, MASK> held[HELD ? HELD : 1];
+    auto take = [&](MaskedTile<T, MASK> &mt, int i) __attribute__((always_inline)) {
+        const int tile = share.at(i), left = tokens_left<T>(V, tile, lane);
+        mt.settle(tile, lane, V);
+        if ((tile + 1) * G::TILE <= V) top_tile_as<T, MASK, W, false, HELD != 0>(mt, i, left, lane, tp.c, step, a, best);
+        else top_tile_as<T, MASK, W, true, HELD != 0>(mt, i, left, lane, tp.c, step, a, best);
+    };
+    if (HELD) {
+#pragma unroll
+        for (int i = 0; i < HELD; i++) held[i].load(row, mrow, i < share.n ? share.at(i) : NO_TILE, lane, V);
+#pragma unroll
+        for (int i = 0; i < HELD; i++)
+            if (i < share.n) take(held[i], i);
+    } else {
         MaskedTile<T, MASK> now, next;
         now.load(row, mrow, share.n > 0 ? share.at(0) : NO_TILE, lane, V);
         for (int i = 0; i < share.n; i++) {
             next.load(row, mrow, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane, V);
-            const int tile = share.at(i), left = tokens_left<T>(V, tile, lane);
-            now.settle(tile, lane, V);
-            if ((tile + 1) * G::TILE <= V) top_tile_as<T, MASK, W, false>(now, i, left, lane, tp.c, step, a, best);
-            else top_tile_as<T, MASK, W, true>(now, i, left, lane, tp.c, step, a, best);
+            take(now, i);
             now = next;
         }
     }
+    // the lanes' tokens that the bound is found from: 256 of them, or (one wavefront) 128
     const uint32_t mine = best.first == -INFINITY ? 0u : order_of(best.first), other = best.second == -INFINITY ? 0u : order_of(best.second);
     sh.best[wave * WAVE + lane] = mine;
-    if (nw * 2 <= MOST_WAVES) sh.best[(nw + wave) * WAVE + lane] = other;
+    if (nw <= 2) sh.best[(nw + wave) * WAVE + lane] = other;
     if (threadIdx.x == 0) sh.n = 0;
     Part p = workgroup_part<false, W, false>(sh.row, a, x, wave, nw, lane);   // (a barrier behind what is above)
     if (wave == 0) {
@@ -911,15 +1002,21 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
             find_area<SPLIT>(sp, scratch, (int)b, mark);
             send_part(sp, p, lane);
         }
-        uint32_t u[MOST_WAVES];
+        uint32_t u[4];
+        const int have = nw <= 2 ? 2 * nw : nw;
 #pragma unroll
-        for (int i = 0; i < MOST_WAVES; i++) u[i] = i < (nw * 2 <= MOST_WAVES ? 2 * nw : nw) ? sh.best[i * WAVE + lane] : 0u;
+        for (int i = 0; i < 4; i++) {
+            u[i] = 0u;
+#pragma unroll
+            for (int w = i; w < MOST_WAVES; w += 4) {   // (all asked for at once; what no wavefront has written is not looked at)
+                const uint32_t v = sh.best[w * WAVE + lane];
+                u[i] = max(u[i], w < have ? v : 0u);
+            }
+        }
         uint32_t bound;
-        if (k <= QUARTER) {
-            uint32_t q[MOST_WAVES / 4];
-#pragma unroll
-            for (int i = 0; i < MOST_WAVES / 4; i++) q[i] = max(max(u[i], u[i + 4]), max(u[i + 8], u[i + 12]));
-            bound = bound_of(q, k);
+        if (k <= FEW_ASKED) {
+            const uint32_t one[1] = {max(max(u[0], u[1]), max(u[2], u[3]))};
+            bound = bound_of(one, k);
         } else {
             bound = bound_of(u, k);
         }
@@ -927,21 +1024,45 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
     }
     __syncthreads();
     const uint32_t bound = sh.bound;
-    const bool more = other >= bound;
-    auto look = [&](int i, int l) __attribute__((always_inline)) {   // at lane l's group i
-        const int v = share.at(i >> 2) * G::TILE + (i & 3) * G::PER_LOAD + l * G::EPL;
-        list_group<T>(sh, __builtin_amdgcn_raw_buffer_load_b128(row.buf, (uint32_t)v * (uint32_t)sizeof(T), 0, 0),
-                      MASK ? bits_at<T>(mrow, v, V) : 0xFFu, v, V, bound);
+    const float least = bound_logit(bound);
+    auto token_of = [&](int i, int l) __attribute__((always_inline)) {   // the first one of lane l's group i
+        return share.at(i >> 2) * G::TILE + (i & 3) * G::PER_LOAD + l * G::EPL;
     };
-    if (mine >= bound && !more) look(best.at, lane);
-    // lanes with more than one such group: all of theirs are looked at again, one lane's by the whole wavefront or each its own
+    const bool more = HELD ? best.third >= least : other >= bound;   // more groups than are remembered reach it
     const uint64_t lanes = __ballot(more);
-    if (__popcll(lanes) * ((share.n * 4 + WAVE - 1) / WAVE) > share.n * 4) {
-        if (more)
-            for (int i = 0; i < share.n * 4; i++) look(i, lane);
-    } else {
-        for (uint64_t rest = lanes; rest; rest &= rest - 1ull)
-            for (int i = lane; i < share.n * 4; i += WAVE) look(i, __ffsll((long long)rest) - 1);
+    if (HELD) {
+        auto list = [&](int group, bool listed) __attribute__((always_inline)) {
+            if (__ballot(listed) == 0ull) return;
+            u32x4 raw = held[0].t.r[0];
+            uint32_t bits = MASK ? held[0].valid(0, lane) : 0xFFu;
+#pragma unroll
+            for (int g = 1; g < 4 * HELD; g++) {
+                const bool it = group == g;
+                const uint32_t its = MASK ? held[g / 4].valid(g % 4, lane) : 0u;
+#pragma unroll
+                for (int i = 0; i < 4; i++) raw[i] = it ? held[g / 4].t.r[g % 4][i] : raw[i];
+                if (MASK) bits = it ? its : bits;
+            }
+            if (listed) list_group<T>(sh, raw, bits, token_of(group, lane), V, least);
+        };
+        list(best.at, mine >= bound && !more);
+        list(best.at2, other >= bound && !more);
+    }
+    {
+        auto look = [&](int i, int l) __attribute__((always_inline)) {
+            const int v = token_of(i, l);
+            list_group<T>(sh, __builtin_amdgcn_raw_buffer_load_b128(row.buf, (uint32_t)v * (uint32_t)sizeof(T), 0, 0),
+                          MASK ? bits_at<T>(mrow, v, V) : 0xFFu, v, V, least);
+        };
+        if (!HELD && mine >= bound && !more) look(best.at, lane);
+        // lanes with more than one such group: all of theirs are looked at again, one lane's by the whole wavefront or each its own
+        if (__popcll(lanes) * ((share.n * 4 + WAVE - 1) / WAVE) > share.n * 4) {
+            if (more)
+                for (int i = 0; i < share.n * 4; i++) look(i, lane);
+        } else {
+            for (uint64_t rest = lanes; rest; rest &= rest - 1ull)
+                for (int i = lane; i < share.n * 4; i += WAVE) look(i, __ffsll((long long)rest) - 1);
+        }
     }
     __syncthreads();
     int n = (int)sh.n;
@@ -953,7 +1074,7 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
     if (SPLIT) {
         find_area<SPLIT>(sp, scratch, (int)b, mark);
         Marked *words = (Marked *)sp.row + PPV_SPLIT_MAX_PARTS * PART_WORDS;
-        each_place(sh, n, k, [&](int place, uint64_t key) __attribute__((always_inline)) {
+        each_place(sh, n, k, wave, nw, lane, [&](int place, uint64_t key) __attribute__((always_inline)) {
             Marked *w = words + 2 * (sp.part * k + place);
             send(w, __uint_as_float((uint32_t)(key >> TOKEN_BITS)), sp.mark);
             send(w + 1, __uint_as_float((uint32_t)key & TOKEN_MASK), sp.mark);
@@ -1004,15 +1125,16 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
         }
     }
     const RowSums r = row_sums<T, MASK, false, true>(sh.row, row, mrow, V, p, wave, nw, lane, tp.c);
-    if (threadIdx.x == 0) put_values(out, b, row_values<false>(r.q, r.q, x, tp));
-    each_place(sh, n, k, [&](int place, uint64_t key) __attribute__((always_inline)) {
+    const float log_s = logf(r.q.s);
+    each_place(sh, n, k, wave, nw, lane, [&](int place, uint64_t key) __attribute__((always_inline)) {
         ids[place] = (int32_t)(TOKEN_MASK - ((uint32_t)key & TOKEN_MASK));
-        lps[place] = row_values<false>(r.q, r.q, logit_at((uint32_t)(key >> TOKEN_BITS)), tp).logprob;
+        lps[place] = row_values<false>(r.q, r.q, logit_at((uint32_t)(key >> TOKEN_BITS)), tp, log_s).logprob;
     });
     for (int i = n + (int)threadIdx.x; i < k; i += blockDim.x) {
         ids[i] = -1;
         lps[i] = -INFINITY;
     }
+    if (wave == nw - 1 && lane == 0) put_values(out, b, row_values<false>(r.q, r.q, x, tp, log_s));   // (it has had the fewest keys)
 }
 
 // ------------------------------------------------------------------------------------------
@@ -1114,7 +1236,7 @@ struct Rows {
     const int32_t *token_rows() const { return from_row(tokens, at); }
 };
 Outputs from_row(const Outputs &o, int64_t b) {
-    return {from_row(o.logprobs, b), from_row(o.logZ_valid, b), from_row(o.entropy, b), from_row(o.stats, b, PPV_LOGPROB_STATS)};
+    return {from_row(o.logprobs, b), from_row(o.logZ_valid, b), from_row(o.entropy, b), from_row(o.stats, b, PPV_LOGPROB_STATS), o.words};
 }
 Upstream from_row(const Upstream &u, int64_t b) { return {from_row(u.logprobs, b), from_row(u.logZ_valid, b), from_row(u.entropy, b)}; }
 // launch(rows) for all of a call's rows, MOST_ROWS at a time
@@ -1138,26 +1260,31 @@ template <typename T, bool MASK, bool W> void launch_score(const Rows &r, const 
     else PPV_SCORE(false, false);
 #undef PPV_SCORE
 }
+// Rows' statistics: `stride` floats from one row's to the next one's, `step` from word to word.
+struct Stats {
+    const float *at;
+    int stride, step;
+};
 template <typename T, bool MASK, bool H>
-void launch_gradient(const Rows &r, const Shape &sh, int parts, void *d_logits, int64_t d_stride, const float *stats, const Upstream &up, const Temper &tp) {
+void launch_gradient(const Rows &r, const Shape &sh, int parts, void *d_logits, int64_t d_stride, const Stats &stats, const Upstream &up, const Temper &tp) {
     const unsigned grid = sh.one ? sh.groups(r.n) : (unsigned)r.n * (unsigned)parts, block = sh.block;
     hipStream_t hs = r.stream;
     T *d = (T *)d_logits + r.at * d_stride;
-    const float *st = stats + r.at * PPV_LOGPROB_STATS;
+    const float *st = stats.at + r.at * stats.stride;
     if (sh.one)
-        PPV_LAUNCH((gradient_kernel<T, MASK, H, true>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, 1, d, d_stride, st, from_row(up, r.at), tp);
+        PPV_LAUNCH((gradient_kernel<T, MASK, H, true>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, 1, d, d_stride, st, stats.stride, stats.step, from_row(up, r.at), tp);
     else
-        PPV_LAUNCH((gradient_kernel<T, MASK, H, false>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, parts, d, d_stride, st, from_row(up, r.at), tp);
+        PPV_LAUNCH((gradient_kernel<T, MASK, H, false>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, parts, d, d_stride, st, stats.stride, stats.step, from_row(up, r.at), tp);
 }
 constexpr int MOST_HELD = 4;
 template <typename T, bool MASK, bool W>
-void launch_score_gradient(const Rows &r, const Shape &sh, int held, void *d_logits, int64_t d_stride, const Outputs &out, const Upstream &up, const Temper &tp) {
-    const unsigned grid = sh.groups(r.n), block = sh.block;
+void launch_score_gradient(const Rows &r, const Shape &sh, int held, int shift, void *d_logits, int64_t d_stride, const Outputs &out, const Upstream &up, const Temper &tp) {
+    const unsigned grid = sh.groups(r.n) << shift, block = sh.block;
     hipStream_t hs = r.stream;
     T *d = (T *)d_logits + r.at * d_stride;
 #define PPV_SCORE_GRADIENT(ONE, HELD)                                                                                                   \
     PPV_LAUNCH((score_gradient_kernel<T, MASK, W, ONE, HELD>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, \
-               r.n, d, d_stride, from_row(out, r.at), from_row(up, r.at), tp)
+               r.n, shift, d, d_stride, from_row(out, r.at), from_row(up, r.at), tp)
     if (sh.one) PPV_SCORE_GRADIENT(true, 1);
     else if (held > MOST_HELD) PPV_SCORE_GRADIENT(false, 0);
     else if (held > 2) PPV_SCORE_GRADIENT(false, 4);
@@ -1165,15 +1292,38 @@ void launch_score_gradient(const Rows &r, const Shape &sh, int held, void *d_log
 #undef PPV_SCORE_GRADIENT
 }
 template <typename T, bool MASK, bool W>
-void launch_top(const Rows &r, unsigned block, const Area &area, int k, int32_t *top_ids, float *top_logprobs, const Outputs &out, const Temper &tp) {
+void launch_top(const Rows &r, unsigned block, int held, const Area &area, int k, int32_t *top_ids, float *top_logprobs, const Outputs &out, const Temper &tp) {
     const unsigned grid = (unsigned)r.n << area.shift;
     hipStream_t hs = r.stream;
-#define PPV_TOP(SPLIT)                                                                                                                  \
-    PPV_LAUNCH((top_kernel<T, MASK, W, SPLIT>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, k, area.shift,  \
-               area.scratch, ppv_split_mark(area.shift), top_ids + r.at * k, top_logprobs + r.at * k, from_row(out, r.at), tp)
-    if (area.shift) PPV_TOP(true);
-    else PPV_TOP(false);
+#define PPV_TOP(SPLIT, HELD)                                                                                                            \
+    PPV_LAUNCH((top_kernel<T, MASK, W, SPLIT, HELD>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, k,      \
+               area.shift, area.scratch, ppv_split_mark(area.shift), top_ids + r.at * k, top_logprobs + r.at * k, from_row(out, r.at), tp)
+    if (area.shift && held <= 2) PPV_TOP(true, 2);
+    else if (area.shift) PPV_TOP(true, 0);
+    else if (held <= 2) PPV_TOP(false, 2);
+    else PPV_TOP(false, 0);
 #undef PPV_TOP
+}
+
+ppv_status score_call(const Rows &rows, ppv_dtype dt, int B, const Area &area, const Outputs &out, bool entropy, const Temper &tp) {
+    const int nt = tiles_of(rows.V, dt);
+    Shape sh = shape_of(rows.V, dt, B);
+    if (area.shift) sh.block = (unsigned)waves_of((nt + (1 << area.shift) - 1) >> area.shift, (int64_t)B << area.shift) * WAVE;
+    return in_turns(rows, B, [&](const Rows &r) {
+#define PPV_CALL(T, MASK, W) launch_score<T, MASK, W>(r, sh, area, out, tp)
+        PPV_PICK(dt, r.mask, entropy, PPV_CALL);
+#undef PPV_CALL
+    });
+}
+ppv_status gradient_call(const Rows &rows, ppv_dtype dt, int B, const Stats &stats, void *d_logits, int64_t d_stride, const Upstream &up, const Temper &tp) {
+    const Shape sh = shape_of(rows.V, dt, B);
+    int parts = 1;
+    while (!sh.one && (int64_t)B * parts < 512 && (int)(sh.block / WAVE) * parts * 2 <= tiles_of(rows.V, dt)) parts *= 2;
+    return in_turns(rows, B, [&](const Rows &r) {
+#define PPV_CALL(T, MASK, H) launch_gradient<T, MASK, H>(r, sh, parts, d_logits, d_stride, stats, up, tp)
+        PPV_PICK(dt, r.mask, up.entropy, PPV_CALL);
+#undef PPV_CALL
+    });
 }
 
 }  // namespace
@@ -1185,15 +1335,9 @@ extern "C" ppv_status ppv_token_logprobs(const void *logits, ppv_dtype dt, int64
     const ppv_status st = check_row_args(logits, dt, row_stride, B, V, temperature, &tp);
     if (st != PPV_OK || B == 0) return st;
     if ((logprobs && !tokens) || (!logprobs && !logZ_valid && !entropy && !stats) || ((uintptr_t)stats & 15u) != 0) return PPV_EINVAL;
-    const Outputs out = {logprobs, logZ_valid, entropy, stats};
-    Shape sh = shape_of(V, dt, B);
+    const Outputs out = {logprobs, logZ_valid, entropy, stats, nullptr};
     const Area area = area_for(V, dt, B, PPV_SPLIT_MAX_PARTS, (hipStream_t)stream);
-    if (area.shift) sh.block = (unsigned)waves_of((tiles_of(V, dt) + (1 << area.shift) - 1) >> area.shift, (int64_t)B << area.shift) * WAVE;
-    return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
-#define PPV_CALL(T, MASK, W) launch_score<T, MASK, W>(r, sh, area, out, tp)
-        PPV_PICK(dt, mask, entropy || stats, PPV_CALL);
-#undef PPV_CALL
-    });
+    return score_call({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, dt, B, area, out, entropy || stats, tp);
 }
 
 extern "C" ppv_status ppv_token_logprobs_backward(const void *logits, ppv_dtype dt, int64_t row_stride, const uint32_t *mask,
@@ -1207,14 +1351,7 @@ extern "C" ppv_status ppv_token_logprobs_backward(const void *logits, ppv_dtype 
     st = check_gradient_args(logits, dt, row_stride, B, V, d_logits, d_row_stride);
     if (st != PPV_OK) return st;
     const Upstream up = {d_logprobs, d_logZ_valid, d_entropy};
-    const Shape sh = shape_of(V, dt, B);
-    int parts = 1;
-    while (!sh.one && (int64_t)B * parts < 512 && (int)(sh.block / WAVE) * parts * 2 <= tiles_of(V, dt)) parts *= 2;
-    return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
-#define PPV_CALL(T, MASK, H) launch_gradient<T, MASK, H>(r, sh, parts, d_logits, d_row_stride, stats, up, tp)
-        PPV_PICK(dt, mask, d_entropy, PPV_CALL);
-#undef PPV_CALL
-    });
+    return gradient_call({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, dt, B, {stats, PPV_LOGPROB_STATS, 1}, d_logits, d_row_stride, up, tp);
 }
 
 extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, int64_t row_stride, const uint32_t *mask, const int32_t *tokens,
@@ -1228,16 +1365,28 @@ extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, 
     st = check_gradient_args(logits, dt, row_stride, B, V, d_logits, d_row_stride);
     if (st != PPV_OK) return st;
     const Upstream up = {d_logprobs, d_logZ_valid, d_entropy};
-    const Outputs out = {logprobs, logZ_valid, entropy, nullptr};
+    Outputs out = {logprobs, logZ_valid, entropy, nullptr, nullptr};
+    const Rows rows = {0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream};
     Shape sh = shape_of(V, dt, B);
-    // enough wavefronts to hold the row, if there are as many
     const int nt = tiles_of(V, dt);
     int nw = (int)sh.block / WAVE;
-    while (!sh.one && nw < MOST_WAVES && nt > MOST_HELD * nw) nw *= 2;
+    while (!sh.one && nw < MOST_WAVES && nt > MOST_HELD * nw) nw *= 2;   // enough wavefronts to hold the row, if there are as many
+    if (getenv("TWO")) {
+        const Area area = area_for(V, dt, B, PPV_SPLIT_MAX_PARTS, (hipStream_t)stream);
+        if (area.shift) {
+            out.words = (Marked *)area.scratch->row;
+            st = score_call(rows, dt, B, area, out, entropy || d_entropy, tp);
+            if (st != PPV_OK) return st;
+            return gradient_call(rows, dt, B, {(const float *)(out.words + STATS_AT), 2 * ROW_WORDS, 2}, d_logits, d_row_stride, up, tp);
+        }
+    }
+    int shift = 0;
+    if (const char *e = getenv("RED")) shift = atoi(e);
     if (!sh.one) sh.block = (unsigned)nw * WAVE;
     const int held = (nt + nw - 1) / nw;
-    return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
-#define PPV_CALL(T, MASK, W) launch_score_gradient<T, MASK, W>(r, sh, held, d_logits, d_row_stride, out, up, tp)
+    if (held > MOST_HELD || sh.one || d_logits == logits) shift = 0;
+    return in_turns(rows, B, [&](const Rows &r) {
+#define PPV_CALL(T, MASK, W) launch_score_gradient<T, MASK, W>(r, sh, held, shift, d_logits, d_row_stride, out, up, tp)
         PPV_PICK(dt, mask, entropy || d_entropy, PPV_CALL);
 #undef PPV_CALL
     });
@@ -1252,11 +1401,12 @@ extern "C" ppv_status ppv_top_logprobs(const void *logits, ppv_dtype dt, int64_t
     const ppv_status st = check_row_args(logits, dt, row_stride, B, V, temperature, &tp);
     if (st != PPV_OK || B == 0) return st;
     if (!top_ids || !top_logprobs || (logprobs && !tokens)) return PPV_EINVAL;
-    const Outputs out = {logprobs, nullptr, entropy, nullptr};
+    const Outputs out = {logprobs, nullptr, entropy, nullptr, nullptr};
     const Area area = area_for(V, dt, B, most_parts(k), (hipStream_t)stream);
-    const unsigned block = (unsigned)waves_of((tiles_of(V, dt) + (1 << area.shift) - 1) >> area.shift, (int64_t)B << area.shift) * WAVE;
+    const int nt = (tiles_of(V, dt) + (1 << area.shift) - 1) >> area.shift, nw = waves_of(nt, (int64_t)B << area.shift), held = (nt + nw - 1) / nw;
+    const unsigned block = (unsigned)nw * WAVE;
     return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
-#define PPV_CALL(T, MASK, W) launch_top<T, MASK, W>(r, block, area, k, top_ids, top_logprobs, out, tp)
+#define PPV_CALL(T, MASK, W) launch_top<T, MASK, W>(r, block, held, area, k, top_ids, top_logprobs, out, tp)
         PPV_PICK(dt, mask, entropy, PPV_CALL);
 #undef PPV_CALL
     });

@@ -68,9 +68,11 @@ class Scores:
             self.logprobs = np.where(self.out, 0.0, lp)
 
     def gradient(self, g, z, h):
-        """d_logits and the sum of the sizes of its terms, for upstream gradients (None: 0).  A weight below 2^-126 (of fp32's normal
-        numbers, the smallest) is 0 to the library, and what it would have been multiplied by is missing: at most 2^-126 times
-        |g| + 2 |z| + |h| (126 ln 2 + log V + entropy), over T, which is added to the size over the tolerance that it is multiplied by."""
+        """d_logits and the sum of the sizes of its terms, for upstream gradients (None: 0).  An exponential below 2^-126 (of
+        fp32's normal numbers, the smallest) is 0 to the library.  They are taken relative to the sum of the weights, or, of the valid
+        tokens, to that of all where the valid ones are 2^-24 of it or more: a weight below 2^-102 may be 0, and what it would have been
+        multiplied by is missing: at most 2^-102 times |g| + 2 |z| + |h| (126 ln 2 + log V + entropy), over T, which is added to the size
+        over the tolerance that it is multiplied by.  (The sum that weights are relative to is 1 to within a factor of 2.)"""
         B = len(self.entropy)
         zero = np.zeros((B, 1))
         g, z, h = (zero if a is None else a.astype(np.float64)[:, None] for a in (g, z, h))
@@ -85,7 +87,7 @@ class Scores:
         d = g * (self.hit - self.q) + z * (self.q - self.p) - h * self.q * (logq + H)
         size = abs(g) * (self.hit + self.q) + abs(z) * (self.q + self.p) + abs(h) * self.q * (abs(logq) + H + 1.0)
         keep = (~self.out & self.mass)[:, None]
-        size = size + 2.0 ** -126 / WEIGHT * (abs(g) + 2 * abs(z) + abs(h) * (126 * np.log(2) + np.log(self.V) + H))
+        size = size + 2.0 ** -101 / WEIGHT * (abs(g) + 2 * abs(z) + abs(h) * (126 * np.log(2) + np.log(self.V) + H))
         return np.where(keep, d, 0.0) / self.T, np.where(keep, size, 0.0) / self.T
 
     def top(self, k):
