@@ -19,12 +19,8 @@ constexpr int SHORT_ROWS = 4;        // rows of one tile: so many to a workgroup
 constexpr float LOWEST = -3.402823466e38f;
 constexpr float FAINT = -1000.f;     // as an exponent of 2: a weight of 0
 
-__device__ __forceinline__ float most(float a, float b) {   // (without the instruction that quiets a NaN first)
-    float r;
-    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-    return r;
-}
-__device__ __forceinline__ float most(float a, float b, float c) {
+__device__ __forceinline__ float most(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float most(float a, float b, float c) {   // (without the instruction that quiets a NaN first)
     float r;
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
@@ -114,20 +110,13 @@ template <int N, bool W> __device__ __forceinline__ void take_few(Tally &a, cons
     }
     add<N, W>(a.few, x, c);
 }
-// A group of a lane's tokens, `bits`: the valid ones.  Where few lanes have any, those are summed by themselves; else with the exponentials
-// that are there, unless a lane's weigh too little against its reference for that.
+// A group of a lane's tokens, `bits`: the valid ones.  Where few lanes have any, and where a lane's weigh too little against its reference, they
+// are left to be summed by themselves (true); else they are summed with the exponentials that are there.
 constexpr int FEW_LANES = 12;
-template <int N, bool MASK, bool W> __device__ __forceinline__ void take_group(Tally &a, float (&x)[N], uint32_t bits, float c, float step) {
+template <int N, bool MASK, bool W> __device__ __forceinline__ bool take_group(Tally &a, const float (&x)[N], uint32_t bits, float c, float step) {
     a.top = most_of<N>(x, a.top);
     raise<MASK>(a, c, step);
-    if (!MASK) {
-        add<N, W>(a.all, x, c);
-        return;
-    }
-    bool alone = bits != 0u;
-    if (__popcll(__ballot(alone)) <= FEW_LANES) {
-        add<N, false>(a.all, x, c);
-    } else {
+    if (MASK && __popcll(__ballot(bits != 0u)) > FEW_LANES) {
         float s = 0.f, w = 0.f;
 #pragma unroll
         for (int i = 0; i < N; i++) {
@@ -137,16 +126,13 @@ template <int N, bool MASK, bool W> __device__ __forceinline__ void take_group(T
             s += v;
             if (W) w = fmaf(most(y, FAINT), v, w);
         }
-        alone = alone && s < FAINT_SUM;
+        const bool alone = s < FAINT_SUM;
         a.s += alone ? 0.f : s;
         if (W) a.w += alone ? 0.f : w;
+        return alone && bits != 0u;
     }
-    if (__ballot(alone) != 0ull) {
-        const uint32_t mine = alone ? bits : 0u;
-#pragma unroll
-        for (int i = 0; i < N; i++) x[i] = if_bit(x[i], mine, i);
-        take_few<N, W>(a, x, c, step);
-    }
+    add<N, W && !MASK>(a.all, x, c);
+    return MASK && bits != 0u;
 }
 
 template <typename T> __device__ __forceinline__ int tiles_in(int V) { return (V + TileGeom<T>::TILE - 1) / TileGeom<T>::TILE; }
@@ -209,45 +195,58 @@ template <typename T> struct Gathered {
 };
 template <typename T, bool MASK, bool W, bool PAD, bool FEW>
 __device__ __forceinline__ void take_groups(const MaskedTile<T, MASK> &mt, int left, int lane, float c, float step, Tally &a) {
+    constexpr int EPL = Elem<T>::EPL;
+    uint32_t alone = 0u;   // the groups whose valid tokens are still to be summed
 #pragma unroll
     for (int j = 0; j < 4; j++) {
-        float x[Elem<T>::EPL];
+        float x[EPL];
         unpack_group<T, PAD>(mt.t.r[j], left - j * TileGeom<T>::PER_LOAD, x);
         if (FEW) {
-            a.top = most_of<Elem<T>::EPL>(x, a.top);
+            a.top = most_of<EPL>(x, a.top);
             raise<true>(a, c, step);
-            add<Elem<T>::EPL, false>(a.all, x, c);
+            add<EPL, false>(a.all, x, c);
         } else {
-            take_group<Elem<T>::EPL, MASK, W>(a, x, mt.valid(j, lane), c, step);
+            alone |= take_group<EPL, MASK, W>(a, x, mt.valid(j, lane), c, step) ? 1u << j : 0u;
         }
         __builtin_amdgcn_sched_barrier(0);   // one group's tokens in registers at a time
+    }
+    if (!FEW && MASK && __ballot(alone != 0u) != 0ull) {
+#pragma unroll 1
+        for (int j = 0; j < 4; j++) {
+            if (__ballot((alone >> j) & 1u) == 0ull) continue;
+            const u32x4 raw = j == 0 ? mt.t.r[0] : j == 1 ? mt.t.r[1] : j == 2 ? mt.t.r[2] : mt.t.r[3];
+            const uint32_t valid = mt.valid(j, lane), bits = (alone >> j) & 1u ? valid : 0u;   // (every lane takes part in the exchange)
+            float x[EPL];
+            unpack_group<T, PAD>(raw, left - j * TileGeom<T>::PER_LOAD, x);
+#pragma unroll
+            for (int i = 0; i < EPL; i++) x[i] = if_bit(x[i], bits, i);
+            take_few<EPL, W>(a, x, c, step);
+        }
     }
 }
 template <typename T, bool MASK, bool W>
 __device__ __forceinline__ void take_tile(const Row &row, const MaskedTile<T, MASK> &mt, int tile, int V, int lane, float c, float step, Tally &a) {
     const int left = tokens_left<T>(V, tile, lane);
     const bool whole = (tile + 1) * TileGeom<T>::TILE <= V;
-    if (MASK) {
-        const uint32_t w = mt.t.word, w2 = w & (w - 1u);
-        a.seen |= w & ~LOST ? 1u : w >> 31;
-        if (__ballot((w2 & (w2 - 1u)) != 0u) == 0ull) {
-            Gathered<T> g;
-            g.load(row, w, tile, lane);
-            if (whole) take_groups<T, MASK, W, false, true>(mt, left, lane, c, step, a);
-            else take_groups<T, MASK, W, true, true>(mt, left, lane, c, step, a);
-            if (__ballot(w != 0u) != 0ull) {
-                const float x0[1] = {w ? g.x[0] : -INFINITY};
-                take_few<1, W>(a, x0, c, step);
-                if (__ballot(w2 != 0u) != 0ull) {
-                    const float x1[1] = {w2 ? g.x[1] : -INFINITY};
-                    take_few<1, W>(a, x1, c, step);
-                }
+    const uint32_t w = MASK ? mt.t.word : 0u, w2 = w & (w - 1u);
+    if (MASK) a.seen |= w & ~LOST ? 1u : w >> 31;
+    if (MASK && __ballot((w2 & (w2 - 1u)) != 0u) == 0ull) {
+        Gathered<T> g;
+        g.load(row, w, tile, lane);
+        if (whole) take_groups<T, MASK, W, false, true>(mt, left, lane, c, step, a);
+        else take_groups<T, MASK, W, true, true>(mt, left, lane, c, step, a);
+        if (__ballot(w != 0u) != 0ull) {
+            const float x0[1] = {w ? g.x[0] : -INFINITY};
+            take_few<1, W>(a, x0, c, step);
+            if (__ballot(w2 != 0u) != 0ull) {
+                const float x1[1] = {w2 ? g.x[1] : -INFINITY};
+                take_few<1, W>(a, x1, c, step);
             }
-            return;
         }
+    } else {
+        if (whole) take_groups<T, MASK, W, false, false>(mt, left, lane, c, step, a);
+        else take_groups<T, MASK, W, true, false>(mt, left, lane, c, step, a);
     }
-    if (whole) take_groups<T, MASK, W, false, false>(mt, left, lane, c, step, a);
-    else take_groups<T, MASK, W, true, false>(mt, left, lane, c, step, a);
 }
 // The wavefront's tiles from its i-th on: the next one is on its way while one is summed.
 template <typename T, bool MASK, bool W>
@@ -550,7 +549,8 @@ __device__ __forceinline__ void put_group(float *row, int v, int V, const float 
     int left = V - v;
     asm volatile("" : "+v"(left));   // (see unpack_group)
     if (left >= 4) {
-        *(float4 *)(row + v) = {d[0], d[1], d[2], d[3]};
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        __builtin_nontemporal_store((f32x4){d[0], d[1], d[2], d[3]}, (f32x4 *)(row + v));
     } else {
 #pragma unroll
         for (int k = 0; k < 3; k++)
@@ -566,7 +566,7 @@ __device__ __forceinline__ void put_group(uint16_t *row, int v, int V, const flo
     int left = V - v;
     asm volatile("" : "+v"(left));
     if (left >= 8) {
-        *(u32x4 *)(row + v) = r;
+        __builtin_nontemporal_store(r, (u32x4 *)(row + v));
     } else {
 #pragma unroll
         for (int k = 0; k < 7; k++)
@@ -1288,7 +1288,8 @@ void launch_score_gradient(const Rows &r, const Shape &sh, int held, int shift, 
     if (sh.one) PPV_SCORE_GRADIENT(true, 1);
     else if (held > MOST_HELD) PPV_SCORE_GRADIENT(false, 0);
     else if (held > 2) PPV_SCORE_GRADIENT(false, 4);
-    else PPV_SCORE_GRADIENT(false, 2);
+    else if (held > 1) PPV_SCORE_GRADIENT(false, 2);
+    else PPV_SCORE_GRADIENT(false, 1);
 #undef PPV_SCORE_GRADIENT
 }
 template <typename T, bool MASK, bool W>
