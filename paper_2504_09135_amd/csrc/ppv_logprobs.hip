@@ -8,7 +8,6 @@
 //   d_l            = d_logprob (1[v = t] - q) + d_logZ (q - p) - d_entropy q (log q + entropy),   d_logits = d_l / T
 // A row is read once, by all lanes of its wavefronts, each with its own running reference and sums relative to it; the lanes' sums are
 // brought to one reference at the end.  Sums are fp32: a lane adds at most 4,096 terms of one sign.
-#include <cstdlib>
 #include "ppv_rows.h"
 #include "ppv_split.h"
 
@@ -867,7 +866,7 @@ __device__ __forceinline__ void top_tile_as(const MaskedTile<T, MASK> &mt, int i
 // wavefront, bit by bit from the first in which they differ.
 constexpr int BOUND_BITS = 12;
 constexpr int FEW_ASKED = 20;   // up to so many candidates the bound is found from 64 tokens: a quarter more tokens reach it
-template <int N> __device__ __forceinline__ uint32_t bound_of(const uint32_t (&u)[N], int k) {
+template <int N, int BITS = BOUND_BITS> __device__ __forceinline__ uint32_t bound_of(const uint32_t (&u)[N], int k) {
     uint32_t hi = 0u, lo = 0u;   // the largest, and the complement of the smallest that is one
     int some = 0;
 #pragma unroll
@@ -882,7 +881,7 @@ template <int N> __device__ __forceinline__ uint32_t bound_of(const uint32_t (&u
     if (hi == lo) return hi;
     const int first = 31 - __builtin_clz(hi ^ lo);
     uint32_t t = hi & ~((2u << first) - 1u);
-    for (int bit = first; bit >= 0 && bit > first - BOUND_BITS; bit--) {
+    for (int bit = first; bit >= 0 && bit > first - BITS; bit--) {
         const uint32_t try_at = t | 1u << bit;
         int n = 0;
 #pragma unroll
@@ -917,6 +916,34 @@ __device__ __forceinline__ void list_group(TopShared &sh, const u32x4 &raw, uint
         } while (m);
     }
 }
+// Takes those of the n listed keys out that are not among the first k, but for ties of the last one's logit.  By one wavefront, in place.
+template <int N> __device__ __forceinline__ int thin_out(TopShared &sh, int n, int k, int lane) {
+    uint32_t u[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) u[i] = i * WAVE + lane < n ? (uint32_t)(sh.list[i * WAVE + lane] >> TOKEN_BITS) : 0u;
+    const uint32_t bound = bound_of<N, 32>(u, k);
+    int kept = 0;
+#pragma unroll 1
+    for (int i = 0; i * WAVE < n; i++) {
+        const uint64_t key = i * WAVE + lane < n ? sh.list[i * WAVE + lane] : 0ull;
+        const bool keep = key >> TOKEN_BITS >= bound;
+        const uint64_t who = __ballot(keep);
+        if (keep) sh.list[kept + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u))] = key;
+        kept += __popcll(who);
+    }
+    return kept;
+}
+// The same where it pays (placing n keys takes n^2 comparisons), by all wavefronts, with a barrier ahead; -1: more than `most` ties are left.
+constexpr int SPARE = 48, MOST_ALIKE = 256;
+__device__ __forceinline__ int thinned_out(TopShared &sh, int n, int k, int most, int wave, int lane) {
+    if (n <= k + SPARE) return n;
+    if (wave == 0) {
+        const int kept = n <= 4 * WAVE ? thin_out<4>(sh, n, k, lane) : thin_out<MOST_LISTED / WAVE>(sh, n, k, lane);
+        if (lane == 0) sh.n = kept <= k + most ? kept : -1;
+    }
+    __syncthreads();
+    return (int)sh.n;
+}
 // The row's first k of n listed keys, by all wavefronts: f(place, key) for each of them, in no order.  A key's place is how many are larger:
 // a wavefront has every nw-th key, one to a lane, and counts for one after the other in as many comparisons as there are 64 keys.
 template <typename F> __device__ __forceinline__ void each_place(const TopShared &sh, int n, int k, int wave, int nw, int lane, F f) {
@@ -926,10 +953,13 @@ template <typename F> __device__ __forceinline__ void each_place(const TopShared
         int place = 0;
         for (int j0 = 0; j0 < n; j0 += WAVE) {
             const uint64_t other = j0 + lane < n ? sh.list[j0 + lane] : 0ull;
-            for (int l = 0; l < mine; l++) {
-                const uint64_t it = (uint64_t)lane_value((uint32_t)(key >> 32), l) << 32 | lane_value((uint32_t)key, l);
-                const int larger = __popcll(__ballot(other > it));
-                place += lane == l ? larger : 0;
+            for (int l0 = 0; l0 < mine; l0 += 4) {   // (four that do not wait for one another)
+#pragma unroll
+                for (int l = l0; l < l0 + 4; l++) {
+                    const uint64_t it = (uint64_t)lane_value((uint32_t)(key >> 32), l) << 32 | lane_value((uint32_t)key, l);
+                    const int larger = __popcll(__ballot(other > it));
+                    place += lane == l ? larger : 0;
+                }
             }
         }
         if (place < k && key) f(place, key);
@@ -1066,7 +1096,9 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
     }
     __syncthreads();
     int n = (int)sh.n;
-    if (n > MOST_LISTED) {   // tokens that are too much alike
+    __syncthreads();
+    if (n <= MOST_LISTED) n = thinned_out(sh, n, k, MOST_ALIKE, wave, lane);
+    if (n > MOST_LISTED || n < 0) {   // tokens that are too much alike
         __syncthreads();
         select_row<T, MASK>(sh, row, mrow, V, k, first, of, wave, nw, lane);
         n = (int)sh.n;
@@ -1123,6 +1155,8 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
             n = 0;
             p.all.s = __uint_as_float(0x7FC00000u);
         }
+        __syncthreads();
+        n = thinned_out(sh, n, k, MOST_LISTED, wave, lane);
     }
     const RowSums r = row_sums<T, MASK, false, true>(sh.row, row, mrow, V, p, wave, nw, lane, tp.c);
     const float log_s = logf(r.q.s);
@@ -1169,14 +1203,27 @@ struct Area {
     int shift;
     SplitScratch *scratch;
 };
-Area area_for(int V, ppv_dtype dt, int B, int most, hipStream_t stream) {
+// More workgroups take more of the row off each and make more to hand over; batches beyond 256 workgroups leave no compute unit idle.
+// us with 1 / 2 / 4 / 8 / 16, bf16 (masks as prefixes have them): scores, V = 32k, 16 rows 6.8 / 6.7 / 6.3 / 6.7 / 6.7, 128 rows 7.0 / 7.5 / 7.7;
+// V = 64k, 1 row 9.7 / 8.3 / 6.7 / 6.4 / 6.6, 64 rows 10.0 / 8.6 / 7.6 / 8.5; V = 128k, 1 row 15.8 / 11.3 / 8.3 / 7.2 / 6.7, 32 rows 16.0 /
+// 11.7 / 8.7 / 7.8 / 9.6, 128 rows 16.5 / 13.1 / 13.5; fp32 without masks, V = 50k, 128 rows 7.9 / 8.4 / 8.9.  Alternatives (20, without masks),
+// V = 64k, 16 rows 10.3 / 10.4 / 10.2 / 14.9; V = 128k, 1 row 13.5 / 11.7 / 10.3 / 11.8, 64 rows 14.6 / 13.0 / 11.9 / 15.6, 128 rows 15.0 / 14.2 /
+// 15.6; V = 256k, 32 rows 22.3 / 17.0 / 13.6 / 13.6; fp32, V = 50k, 128 rows 10.9 / 11.8 / 13.6.
+// Every part's candidates are placed among those of all.  (V = 128k, 1 row, unsplit / in 4 / 8: 5 of them 12.8 / 9.4 / 8.4, 50
+// of them 13.7 / 12.8 / 14.2, 128 of them 18.2 / 24.3; V = 64k 8.6 / 8.1 / 8.0, 10.3 / 11.8 / 17.1, 14.4 / 23.1.)
+Area area_for(int V, ppv_dtype dt, int B, int k, int most, hipStream_t stream) {   // k: alternatives, 0 for scores
     const int nt = tiles_of(V, dt);
     int shift = 0;
     if (B <= PPV_SPLIT_MAX_ROWS) {
         if (const int v = ppv_tuning(PPV_TUNE_ROW_SPLIT)) {
             while ((2 << shift) <= v) shift++;
         } else {
-            while ((B << (shift + 1)) <= 256 && (1 << (shift + 1)) <= PPV_SPLIT_MAX_PARTS && nt >> (shift + 1) >= 4) shift++;
+            auto pays = [&](int parts) {
+                if (B * parts > 256) return false;
+                if (k) return parts <= 8 && parts * k <= 200 && (k <= 24 || nt >= 60) && nt / parts >= (B > 64 ? 28 : (k <= 8 ? 7 : 12));
+                return nt / parts >= (B > 64 ? 16 : (parts >= 8 && B > 4 ? 6 : 4)) && (parts < 16 || B <= 4);
+            };
+            while ((2 << shift) <= PPV_SPLIT_MAX_PARTS && pays(2 << shift)) shift++;
         }
         while (shift && ((1 << shift) > most || 2 << shift > nt)) shift--;   // two tiles each
     }
@@ -1317,7 +1364,11 @@ ppv_status score_call(const Rows &rows, ppv_dtype dt, int B, const Area &area, c
     });
 }
 ppv_status gradient_call(const Rows &rows, ppv_dtype dt, int B, const Stats &stats, void *d_logits, int64_t d_stride, const Upstream &up, const Temper &tp) {
-    const Shape sh = shape_of(rows.V, dt, B);
+    Shape sh = shape_of(rows.V, dt, B);
+    // (large batches: us with 4 / 8 / 16 wavefronts, V = 32k bf16, 2,048 rows 51.5 / 49.5 / 46.7, V = 128k, 1,024 rows 104.4 / 102.6 / 99.1; but
+    // 256 rows at V = 32k 7.7 with 4 and 8.3 with 16)
+    if (!sh.one && B >= 512)
+        while ((int)(sh.block / WAVE) * 2 <= tiles_of(rows.V, dt) && sh.block < MOST_WAVES * WAVE) sh.block *= 2;
     int parts = 1;
     while (!sh.one && (int64_t)B * parts < 512 && (int)(sh.block / WAVE) * parts * 2 <= tiles_of(rows.V, dt)) parts *= 2;
     return in_turns(rows, B, [&](const Rows &r) {
@@ -1337,7 +1388,7 @@ extern "C" ppv_status ppv_token_logprobs(const void *logits, ppv_dtype dt, int64
     if (st != PPV_OK || B == 0) return st;
     if ((logprobs && !tokens) || (!logprobs && !logZ_valid && !entropy && !stats) || ((uintptr_t)stats & 15u) != 0) return PPV_EINVAL;
     const Outputs out = {logprobs, logZ_valid, entropy, stats, nullptr};
-    const Area area = area_for(V, dt, B, PPV_SPLIT_MAX_PARTS, (hipStream_t)stream);
+    const Area area = area_for(V, dt, B, 0, PPV_SPLIT_MAX_PARTS, (hipStream_t)stream);
     return score_call({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, dt, B, area, out, entropy || stats, tp);
 }
 
@@ -1372,8 +1423,12 @@ extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, 
     const int nt = tiles_of(V, dt);
     int nw = (int)sh.block / WAVE;
     while (!sh.one && nw < MOST_WAVES && nt > MOST_HELD * nw) nw *= 2;   // enough wavefronts to hold the row, if there are as many
-    if (getenv("TWO")) {
-        const Area area = area_for(V, dt, B, PPV_SPLIT_MAX_PARTS, (hipStream_t)stream);
+    const int held = (nt + nw - 1) / nw;
+    // Few rows that no workgroup can hold, or not without long work on their masks: the sums by several workgroups, then the gradient.  (us
+    // in one launch / in two, 32 rows: V = 100k fp32 25.0 / 17.3, masked 31.9 / 19.1; V = 128k bf16 masked 29.4 / 18.7, but without a mask
+    // 16.2 / 16.2 and V = 64k masked 14.5 / 14.2, V = 50k fp32 masked 15.6 / 16.3.)
+    if (held > MOST_HELD || (mask && V >= 96000)) {
+        const Area area = area_for(V, dt, B, 0, PPV_SPLIT_MAX_PARTS, (hipStream_t)stream);
         if (area.shift) {
             out.words = (Marked *)area.scratch->row;
             st = score_call(rows, dt, B, area, out, entropy || d_entropy, tp);
@@ -1381,11 +1436,12 @@ extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, 
             return gradient_call(rows, dt, B, {(const float *)(out.words + STATS_AT), 2 * ROW_WORDS, 2}, d_logits, d_row_stride, up, tp);
         }
     }
+    // Two or four workgroups to a row of a small batch.  (us with one / two / four, V = 32k bf16 masked: 32 rows 11.1 / 10.0 / 9.6, 64 rows 11.1 /
+    // 10.2 / 10.3, 128 rows 11.3 / 10.9 / 17.6; without masks 7.8 / 7.2 / 7.1, 8.1 / 7.4 / 7.6, 8.1 / 8.1 / 13.0.)  They read the whole
+    // row: not where another one writes it.
     int shift = 0;
-    if (const char *e = getenv("RED")) shift = atoi(e);
+    while (!sh.one && held <= MOST_HELD && d_logits != logits && shift < 2 && nt >= 8 && (B << (shift + 1)) <= 128) shift++;
     if (!sh.one) sh.block = (unsigned)nw * WAVE;
-    const int held = (nt + nw - 1) / nw;
-    if (held > MOST_HELD || sh.one || d_logits == logits) shift = 0;
     return in_turns(rows, B, [&](const Rows &r) {
 #define PPV_CALL(T, MASK, W) launch_score_gradient<T, MASK, W>(r, sh, held, shift, d_logits, d_row_stride, out, up, tp)
         PPV_PICK(dt, mask, entropy || d_entropy, PPV_CALL);
@@ -1403,7 +1459,7 @@ extern "C" ppv_status ppv_top_logprobs(const void *logits, ppv_dtype dt, int64_t
     if (st != PPV_OK || B == 0) return st;
     if (!top_ids || !top_logprobs || (logprobs && !tokens)) return PPV_EINVAL;
     const Outputs out = {logprobs, nullptr, entropy, nullptr, nullptr};
-    const Area area = area_for(V, dt, B, most_parts(k), (hipStream_t)stream);
+    const Area area = area_for(V, dt, B, k, most_parts(k), (hipStream_t)stream);
     const int nt = (tiles_of(V, dt) + (1 << area.shift) - 1) >> area.shift, nw = waves_of(nt, (int64_t)B << area.shift), held = (nt + nw - 1) / nw;
     const unsigned block = (unsigned)nw * WAVE;
     return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
