@@ -440,6 +440,23 @@ __device__ __forceinline__ void put_values(const Outputs &o, int64_t b, const Ro
     if (o.entropy) o.entropy[b] = v.entropy;
 }
 
+template <bool SPLIT> __device__ __forceinline__ Split part_of(unsigned at_place, int shift) {
+    if (!SPLIT) return {1, 0, nullptr, nullptr, 0u};
+    return {1 << shift, (int)(at_place & ((1u << shift) - 1u)), nullptr, nullptr, 0u};
+}
+// Workgroup `group` of `groups` takes the place() -th piece of work.  Neighbouring workgroups start on the chip's eight dies in turn; a batch
+// often has a period (a query's candidates, a sequence's positions), and rows of one kind, those near the root with long work on their
+// masks, would all meet on one die.  So each die has a
+// stretch of its own, and each round of its compute units starts at another place.  (Scores under masks, every
+// eighth row near the root, us in turn / so: 1,024 rows at V = 256k bf16 96.7 / 92.9 with four wavefronts, 4,096 at V = 32k 53.1 / 49.2.)
+constexpr unsigned DIES = 8, DIE_UNITS = 32;
+__device__ __forceinline__ unsigned place(unsigned group, unsigned groups) {
+    const unsigned die = group % DIES, each = groups / DIES, more = groups % DIES, mine = each + (die < more ? 1u : 0u);
+    unsigned i = group / DIES;
+    const unsigned round = i / DIE_UNITS;
+    if ((round + 1u) * DIE_UNITS <= mine) i = round * DIE_UNITS + (i + 5u * round) % DIE_UNITS;
+    return die * each + min(die, more) + i;
+}
 // ------------------------------------------------------------------------------------------
 // Forward.  ONE: rows of one tile, a wavefront each; else a workgroup has a row, or (SPLIT) 1 << shift of them have.
 template <typename T, bool MASK, bool W, bool ONE, bool SPLIT>
@@ -449,9 +466,10 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
                                                                                          Outputs out, Temper tp) {
     __shared__ RowShared sh;
     const int lane = threadIdx.x & (WAVE - 1), wave = ONE ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = ONE ? 1 : blockDim.x / WAVE;
-    const int64_t b = ONE ? (int64_t)blockIdx.x * SHORT_ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) : blockIdx.x >> (SPLIT ? shift : 0);
+    const unsigned at_place = place(blockIdx.x, gridDim.x);
+    const int64_t b = ONE ? (int64_t)at_place * SHORT_ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) : at_place >> (SPLIT ? shift : 0);
     if (ONE && b >= B) return;
-    Split sp = split_of<SPLIT>(shift);
+    Split sp = part_of<SPLIT>(at_place, shift);
     const int tok = tokens ? tokens[b] : V;
     if (tok < 0) {   // left out
         if (lane == 0 && wave == 0 && sp.part == 0) {
@@ -631,45 +649,44 @@ template <typename T> __device__ __forceinline__ void put_zeros(T *out, int firs
 #pragma unroll
         for (int j = 0; j < 4; j++) put_group(out, t * G::TILE + j * G::PER_LOAD + lane * G::EPL, V, d);
 }
-// The wavefront's tiles from its i-th on; each is read before another one is written: out may be the logits themselves.
+// The wavefront's tiles, the first of them asked for; each is read before another one is written: out may be the logits themselves.
 template <typename T, bool MASK, bool H>
-__device__ __forceinline__ void put_tiles(T *out, const Row &row, const uint32_t *mask, const Slope &s, int tok, int V, const Share &share, int i, int lane, float c) {
-    if (i >= share.n) return;
-    MaskedTile<T, MASK> now, next;
-    now.load(row, mask, share.at(i), lane, V);
-    for (; i < share.n; i++) {
+__device__ __forceinline__ void put_tiles(T *out, const Row &row, const uint32_t *mask, MaskedTile<T, MASK> &now, const Slope &s, int tok, int V, const Share &share, int lane, float c) {
+    MaskedTile<T, MASK> next;
+    for (int i = 0; i < share.n; i++) {
         next.load(row, mask, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane, V);
         now.settle(share.at(i), lane, V);
         put_tile<T, MASK, H>(out, now, s, share.at(i), lane, tok, V, c);
         now = next;
     }
 }
-// `parts` workgroups to a row; SHORT_ROWS rows to a workgroup where a row is one tile.
+// 1 << shift workgroups to a row; SHORT_ROWS rows to a workgroup where a row is one tile.
 template <typename T, bool MASK, bool H, bool ONE>
 __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void gradient_kernel(const T *logits, int64_t row_stride, const int32_t *__restrict__ tokens,
-                                                                                            const uint32_t *__restrict__ mask, int V, int n_words, int B, int parts,
+                                                                                            const uint32_t *__restrict__ mask, int V, int n_words, int B, int shift,
                                                                                             T *d_logits, int64_t d_row_stride, const float *__restrict__ stats,
                                                                                             int stats_stride, int stats_step, Upstream up, Temper tp) {
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = blockDim.x / WAVE;
-    const int64_t units = ONE ? B : (int64_t)B * parts;
-    const int per = ONE ? SHORT_ROWS : 1;
-    const int64_t u = (int64_t)blockIdx.x * per + (ONE ? wave : 0);
-    if (u < units) {
-        const int64_t b = ONE ? u : u / parts;
-        const int part = ONE ? 0 : (int)(u - b * parts);
-        const int tok = tokens ? tokens[b] : V;
-        const float *st = stats + b * stats_stride;   // (in the rows' scratch a word is a float and a mark)
-        const Sums all = {st[0], st[stats_step], 0.f}, q = {st[2 * stats_step], st[3 * stats_step], 0.f};
-        const Slope s = slope_of<MASK>(all, q, st[4 * stats_step], st[5 * stats_step], up, b, tok, tp);
-        T *to = d_logits + b * d_row_stride;
-        const int first = ONE ? 0 : part * nw + wave, of = ONE ? 1 : nw * parts;
-        if (s.nothing) {
-            put_zeros(to, first, of, lane, V);
-            return;
-        }
-        const Row row = row_of(logits + b * row_stride, V);
-        put_tiles<T, MASK, H>(to, row, MASK ? mask + b * n_words : nullptr, s, tok, V, share_of(tiles_in<T>(V), first, of), 0, lane, tp.c);
+    const unsigned at_place = place(blockIdx.x, gridDim.x);
+    const int64_t b = ONE ? (int64_t)at_place * SHORT_ROWS + wave : at_place >> shift;
+    if (ONE && b >= B) return;
+    const int first = ONE ? 0 : (int)(at_place & ((1u << shift) - 1u)) * nw + wave, of = ONE ? 1 : nw << shift;
+    const int tok = tokens ? tokens[b] : V;
+    T *to = d_logits + b * d_row_stride;
+    if (tok < 0) {   // left out
+        put_zeros(to, first, of, lane, V);
+        return;
     }
+    const Row row = row_of(logits + b * row_stride, V);
+    const uint32_t *mrow = MASK ? mask + b * n_words : nullptr;
+    const Share share = share_of(tiles_in<T>(V), first, of);
+    MaskedTile<T, MASK> tile;   // (asked for ahead of what the slopes are made of)
+    tile.load(row, mrow, share.n > 0 ? share.at(0) : NO_TILE, lane, V);
+    const float *st = stats + b * stats_stride;   // (in the rows' scratch a word is a float and a mark)
+    const Sums all = {st[0], st[stats_step], 0.f}, q = {st[2 * stats_step], st[3 * stats_step], 0.f};
+    const Slope s = slope_of<MASK>(all, q, st[4 * stats_step], st[5 * stats_step], up, b, tok, tp);
+    if (s.nothing) put_zeros(to, first, of, lane, V);
+    else put_tiles<T, MASK, H>(to, row, mrow, tile, s, tok, V, share, lane, tp.c);
 }
 
 // Both: the sums, then the gradient.  A wavefront holds its tiles, at most HELD; HELD = 0: they are read again.  1 << shift workgroups may
@@ -680,9 +697,10 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
                                                                                                   T *d_logits, int64_t d_row_stride, Outputs out, Upstream up, Temper tp) {
     __shared__ RowShared sh;
     const int lane = threadIdx.x & (WAVE - 1), wave = ONE ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = ONE ? 1 : blockDim.x / WAVE;
-    const int64_t b = ONE ? (int64_t)blockIdx.x * SHORT_ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) : blockIdx.x >> shift;
+    const unsigned at_place = place(blockIdx.x, gridDim.x);
+    const int64_t b = ONE ? (int64_t)at_place * SHORT_ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE) : at_place >> shift;
     if (ONE && b >= B) return;
-    const int part = ONE ? 0 : blockIdx.x & ((1 << shift) - 1);
+    const int part = ONE ? 0 : at_place & ((1 << shift) - 1);
     const int tok = tokens ? tokens[b] : V;
     T *to = d_logits + b * d_row_stride;
     if (tok < 0) {   // left out
@@ -719,7 +737,10 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
 #pragma unroll
     for (int i = 0; i < HELD; i++)   // (four neighbouring wavefronts' tiles are one part's: those of the four SIMDs)
         if (i < share.n && (ONE || ((share.at(i) >> 2) & ((1 << shift) - 1)) == part)) put_tile<T, MASK, W>(to, held[i], s, share.at(i), lane, tok, V, tp.c);
-    if (HELD == 0) put_tiles<T, MASK, W>(to, row, mrow, s, tok, V, share, 0, lane, tp.c);
+    if (HELD == 0) {
+        held[0].load(row, mrow, share.n > 0 ? share.at(0) : NO_TILE, lane, V);
+        put_tiles<T, MASK, W>(to, row, mrow, held[0], s, tok, V, share, lane, tp.c);
+    }
 }
 
 // ------------------------------------------------------------------------------------------
@@ -976,8 +997,9 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
     using G = TileGeom<T>;
     __shared__ TopShared sh;
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = blockDim.x / WAVE;
-    const int64_t b = blockIdx.x >> (SPLIT ? shift : 0);
-    Split sp = split_of<SPLIT>(shift);
+    const unsigned at_place = place(blockIdx.x, gridDim.x);
+    const int64_t b = at_place >> (SPLIT ? shift : 0);
+    Split sp = part_of<SPLIT>(at_place, shift);
     const int tok = tokens ? tokens[b] : V;
     int32_t *ids = top_ids + b * k;
     float *lps = top_logprobs + b * k;
@@ -1313,15 +1335,15 @@ struct Stats {
     int stride, step;
 };
 template <typename T, bool MASK, bool H>
-void launch_gradient(const Rows &r, const Shape &sh, int parts, void *d_logits, int64_t d_stride, const Stats &stats, const Upstream &up, const Temper &tp) {
-    const unsigned grid = sh.one ? sh.groups(r.n) : (unsigned)r.n * (unsigned)parts, block = sh.block;
+void launch_gradient(const Rows &r, const Shape &sh, int shift, void *d_logits, int64_t d_stride, const Stats &stats, const Upstream &up, const Temper &tp) {
+    const unsigned grid = sh.one ? sh.groups(r.n) : (unsigned)r.n << shift, block = sh.block;
     hipStream_t hs = r.stream;
     T *d = (T *)d_logits + r.at * d_stride;
     const float *st = stats.at + r.at * stats.stride;
     if (sh.one)
-        PPV_LAUNCH((gradient_kernel<T, MASK, H, true>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, 1, d, d_stride, st, stats.stride, stats.step, from_row(up, r.at), tp);
+        PPV_LAUNCH((gradient_kernel<T, MASK, H, true>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, 0, d, d_stride, st, stats.stride, stats.step, from_row(up, r.at), tp);
     else
-        PPV_LAUNCH((gradient_kernel<T, MASK, H, false>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, parts, d, d_stride, st, stats.stride, stats.step, from_row(up, r.at), tp);
+        PPV_LAUNCH((gradient_kernel<T, MASK, H, false>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, shift, d, d_stride, st, stats.stride, stats.step, from_row(up, r.at), tp);
 }
 constexpr int MOST_HELD = 4;
 template <typename T, bool MASK, bool W>
@@ -1365,14 +1387,16 @@ ppv_status score_call(const Rows &rows, ppv_dtype dt, int B, const Area &area, c
 }
 ppv_status gradient_call(const Rows &rows, ppv_dtype dt, int B, const Stats &stats, void *d_logits, int64_t d_stride, const Upstream &up, const Temper &tp) {
     Shape sh = shape_of(rows.V, dt, B);
-    // (large batches: us with 4 / 8 / 16 wavefronts, V = 32k bf16, 2,048 rows 51.5 / 49.5 / 46.7, V = 128k, 1,024 rows 104.4 / 102.6 / 99.1; but
-    // 256 rows at V = 32k 7.7 with 4 and 8.3 with 16)
-    if (!sh.one && B >= 512)
-        while ((int)(sh.block / WAVE) * 2 <= tiles_of(rows.V, dt) && sh.block < MOST_WAVES * WAVE) sh.block *= 2;
-    int parts = 1;
-    while (!sh.one && (int64_t)B * parts < 512 && (int)(sh.block / WAVE) * parts * 2 <= tiles_of(rows.V, dt)) parts *= 2;
+    // No wavefront waits for another here.  us with 4 / 8 / 16 wavefronts, bf16: V = 32k, 64 rows 4.7 / 4.9 / 6.6, 2,048 rows 51.5 / 49.5 / 46.7;
+    // V = 128k, 16 rows 4.6 / 5.2 / 7.5, 1,024 rows 104.4 / 102.6 / 99.1; V = 50k fp32, 128 rows 11.6 / 12.1 / 12.2, 400 rows 36.6 / 35.0 / 35.5.
+    int nw = B < 256 ? 4 : (B < 512 ? 8 : MOST_WAVES);
+    if (const int v = ppv_tuning(PPV_TUNE_WAVES_PER_ROW)) nw = v;
+    while (nw > tiles_of(rows.V, dt) || (nw & (nw - 1))) nw--;
+    if (!sh.one) sh.block = (unsigned)nw * WAVE;
+    int shift = 0;
+    while (!sh.one && (int64_t)B << shift < 512 && (int)(sh.block / WAVE) << (shift + 1) <= tiles_of(rows.V, dt)) shift++;
     return in_turns(rows, B, [&](const Rows &r) {
-#define PPV_CALL(T, MASK, H) launch_gradient<T, MASK, H>(r, sh, parts, d_logits, d_stride, stats, up, tp)
+#define PPV_CALL(T, MASK, H) launch_gradient<T, MASK, H>(r, sh, shift, d_logits, d_stride, stats, up, tp)
         PPV_PICK(dt, r.mask, up.entropy, PPV_CALL);
 #undef PPV_CALL
     });
