@@ -763,11 +763,11 @@ __device__ __forceinline__ uint64_t key_of(float x, int v) {
 constexpr int MOST_LISTED = 1024;   // candidates not below the bound that are sorted out in LDS
 struct TopShared {
     RowShared row;
-    union {
+    union {   // one after the other, with a barrier between
         uint32_t best[MOST_WAVES * WAVE];   // each lane's largest token, and (up to two wavefronts) the largest of its other groups
         uint32_t bin[BINS];
+        uint64_t list[MOST_LISTED];
     };
-    uint64_t list[MOST_LISTED];
     uint64_t prefix;
     uint32_t n, want, bound;
     int settled;
@@ -966,8 +966,19 @@ __device__ __forceinline__ int thinned_out(TopShared &sh, int n, int k, int most
     return (int)sh.n;
 }
 // The row's first k of n listed keys, by all wavefronts: f(place, key) for each of them, in no order.  A key's place is how many are larger:
-// a wavefront has every nw-th key, one to a lane, and counts for one after the other in as many comparisons as there are 64 keys.
+// a wavefront has every nw-th key, one to a lane, and counts for one after the other in as many comparisons as there are 64 keys; or, one or
+// two wavefronts, each lane counts for its own.
 template <typename F> __device__ __forceinline__ void each_place(const TopShared &sh, int n, int k, int wave, int nw, int lane, F f) {
+    if (nw <= 2) {
+        for (int i = wave * WAVE + lane; i < n; i += nw * WAVE) {
+            const uint64_t key = sh.list[i];
+            int place = 0;
+#pragma unroll 8
+            for (int j = 0; j < n; j++) place += sh.list[j] > key;
+            if (place < k && key) f(place, key);
+        }
+        return;
+    }
     for (int i0 = wave; i0 < n; i0 += nw * WAVE) {
         const int i = i0 + lane * nw, mine = min((n - i0 + nw - 1) / nw, WAVE);
         const uint64_t key = i < n ? sh.list[i] : 0ull;
@@ -1199,9 +1210,14 @@ int tiles_of(int V, ppv_dtype dt) {
     const int tile = dt == PPV_F32 ? TileGeom<float>::TILE : TileGeom<uint16_t>::TILE;
     return (V + tile - 1) / tile;
 }
-// Wavefronts per row: a power of two, at most one per tile.
-int waves_of(int nt, int64_t rows) {
+// Wavefronts per row: a power of two.  A small batch is over when its longest row is, a large one when the chip's issue slots or the memory are
+// through with all of them; each wavefront takes part in what follows the pass over a row.  us with 1 / 2 / 4 / 8 / 16: scores under
+// prefixes' masks, bf16, V = 8k, 300 rows 8.9 / 7.3 / 5.9 / 5.8, 4,000 rows 19.8 / 18.8 / 19.4; V = 32k, 4,096 rows 54.7 (two) / 49.2 / 55.6 / 100;
+// V = 256k, 1,024 rows 92.9 (four) / 92.7 / 107; fp32, V = 2,100 (three tiles), 4,000 rows 12.6 / 13.1 / 15.8.  Alternatives, V = 3,224 bf16,
+// 4,000 rows 12.6 / 13.4; V = 8k 18.6 / 19.0 / 21.4; 300 rows 9.4 / 8.0 / 7.1 / 7.0.
+int waves_of(int nt, int64_t rows, bool top = false) {
     int cap = rows <= 256 ? 16 : (nt >= 48 || rows <= 512 ? 8 : 4);
+    if (rows >= 2048 && nt <= 4) cap = nt <= 3 ? 1 : (top ? 2 : 4);
     if (const int v = ppv_tuning(PPV_TUNE_WAVES_PER_ROW)) cap = v;
     int nw = 1;
     while (nw < nt && nw * 2 <= cap) nw <<= 1;
@@ -1484,7 +1500,7 @@ extern "C" ppv_status ppv_top_logprobs(const void *logits, ppv_dtype dt, int64_t
     if (!top_ids || !top_logprobs || (logprobs && !tokens)) return PPV_EINVAL;
     const Outputs out = {logprobs, nullptr, entropy, nullptr, nullptr};
     const Area area = area_for(V, dt, B, k, most_parts(k), (hipStream_t)stream);
-    const int nt = (tiles_of(V, dt) + (1 << area.shift) - 1) >> area.shift, nw = waves_of(nt, (int64_t)B << area.shift), held = (nt + nw - 1) / nw;
+    const int nt = (tiles_of(V, dt) + (1 << area.shift) - 1) >> area.shift, nw = waves_of(nt, (int64_t)B << area.shift, true), held = (nt + nw - 1) / nw;
     const unsigned block = (unsigned)nw * WAVE;
     return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
 #define PPV_CALL(T, MASK, W) launch_top<T, MASK, W>(r, block, held, area, k, top_ids, top_logprobs, out, tp)
