@@ -519,16 +519,17 @@ struct Upstream {
 };
 // d_logits = e (a + b y) for valid tokens, less e_p z for all of them (a mask, and a slope of log Z), and `at_token` more at the row's token:
 //   TOGETHER   y = x c - r, e = e_p = 2^y with r the reference of all tokens: one exponential a token.  For rows whose valid tokens weigh
-//              2^-TOGETHER_MOST or more of all
+//              enough against all: their exponents are as far below 0 then, and rounded as much more coarsely (2^-24 off for 2^-24 of the
+//              weight is 1e-6, nothing to a gradient in bf16 but more than one in fp32 is rounded by: 2^-4)
 //   else       y and e relative to the valid tokens' reference r, e_p = 2^(x c - rp)
 // In rows beyond FAR_OFF, r and rp are logits, and y = (x - r) c.
-constexpr float TOGETHER_MOST = 24.f;
+template <typename T> constexpr float TOGETHER_MOST = sizeof(T) == 4 ? 4.f : 24.f;
 struct Slope {
     float r, a, b, rp, z, at_token;
     bool nothing;   // zeros all over the row
     bool far, together;
 };
-template <bool MASK> __device__ __forceinline__ Slope slope_of(const Sums &all, const Sums &q, float entropy, float logprob, const Upstream &up, int64_t b, int tok, const Temper &tp) {
+template <typename T, bool MASK> __device__ __forceinline__ Slope slope_of(const Sums &all, const Sums &q, float entropy, float logprob, const Upstream &up, int64_t b, int tok, const Temper &tp) {
     Slope s;
     const float g = up.logprobs && logprob > -INFINITY ? up.logprobs[b] : 0.f;   // (a log probability of -inf has no slope)
     const float z = MASK && up.logZ_valid ? up.logZ_valid[b] : 0.f, h = up.entropy ? up.entropy[b] : 0.f;
@@ -546,7 +547,7 @@ template <bool MASK> __device__ __forceinline__ Slope slope_of(const Sums &all, 
         s.rp = all.m * c;
         float d = fmaf(-q.m, c, s.r);
         if (MASK) {
-            s.together = __builtin_amdgcn_readfirstlane(s.z != 0.f && s.rp - s.r <= TOGETHER_MOST);
+            s.together = __builtin_amdgcn_readfirstlane(s.z != 0.f && s.rp - s.r <= TOGETHER_MOST<T>);
             if (s.together) {
                 d += s.rp - s.r;
                 s.r = s.rp;
@@ -684,7 +685,7 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void gra
     tile.load(row, mrow, share.n > 0 ? share.at(0) : NO_TILE, lane, V);
     const float *st = stats + b * stats_stride;   // (in the rows' scratch a word is a float and a mark)
     const Sums all = {st[0], st[stats_step], 0.f}, q = {st[2 * stats_step], st[3 * stats_step], 0.f};
-    const Slope s = slope_of<MASK>(all, q, st[4 * stats_step], st[5 * stats_step], up, b, tok, tp);
+    const Slope s = slope_of<T, MASK>(all, q, st[4 * stats_step], st[5 * stats_step], up, b, tok, tp);
     if (s.nothing) put_zeros(to, first, of, lane, V);
     else put_tiles<T, MASK, H>(to, row, mrow, tile, s, tok, V, share, lane, tp.c);
 }
@@ -729,7 +730,7 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
     const RowSums r = row_sums<T, MASK, ONE>(sh, row, mrow, V, p, wave, nw, lane, tp.c);
     const RowValues v = row_values<MASK>(r.all, r.q, x, tp);
     if (lane == 0 && wave == 0 && part == 0) put_values(out, b, v);
-    const Slope s = slope_of<MASK>(r.all, r.q, v.entropy, v.logprob, up, b, tok, tp);
+    const Slope s = slope_of<T, MASK>(r.all, r.q, v.entropy, v.logprob, up, b, tok, tp);
     if (s.nothing) {
         put_zeros(to, part * nw + wave, ONE ? 1 : nw << shift, lane, V);
         return;
