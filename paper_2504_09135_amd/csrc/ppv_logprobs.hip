@@ -45,7 +45,7 @@ __device__ __forceinline__ float uniform(float x) { return __int_as_float(__buil
 constexpr float FAR_OFF = 134217728.f;   // 2^27: below it the rounding of r is at most four units of the exponent
 constexpr float RAISE = 12.f;            // units of the exponent; entropies lose 12 * 2^-24 where a row's largest token comes late
 constexpr float FAINT_SUM = 9.09494702e-13f;   // 2^-40: valid tokens that weigh less than that against the lane's reference get one of their own
-constexpr float LOSES = -60.f;           // raised by more than that at once, the valid tokens before may be lost: the careful form again
+constexpr float LOSING = 5.42101086e-20f;      // 2^-64: valid tokens that have come to weigh less, as the reference was raised, may be lost soon: the careful form again
 constexpr uint32_t LOST = 1u << 31;
 struct Run {
     float r, s, w;
@@ -77,9 +77,12 @@ template <bool MASK> __device__ __forceinline__ void raise(Tally &a, float c, fl
     if (__ballot(a.top > a.limit) != 0ull) {
         const bool up = a.top > a.limit;
         const float r = up ? reference_at(a.top, c) : a.all.r, d = a.all.r - r;
-        if (MASK) a.seen |= a.s != 0.f && d < LOSES ? LOST : 0u;
         refer(a.all.s, a.all.w, d);
-        if (MASK) refer(a.s, a.w, d);
+        if (MASK) {
+            const bool some = a.s != 0.f;
+            refer(a.s, a.w, d);
+            a.seen |= some && a.s < LOSING ? LOST : 0u;
+        }
         a.all.r = r;
         a.limit = up ? a.top + step : a.limit;
     }
@@ -415,8 +418,9 @@ struct RowValues {
 // what the sums say.  Without mass (no valid token, or all at -inf): -inf, and an entropy of 0.
 template <bool MASK> __device__ __forceinline__ RowValues row_values(const Sums &all, const Sums &q, float x, const Temper &tp, float log_s) {
     if (!(q.s != 0.f)) return {-INFINITY, -INFINITY, 0.f};
-    return {(x - q.m) * tp.inv - log_s, MASK ? fmaf(q.m - all.m, tp.inv, log_s - logf(all.s)) : 0.f,
-            fmaxf(fmaf(q.w / q.s, -LN2F, log_s), 0.f)};
+    const float logprob = (x - q.m) * tp.inv - log_s, logZ = MASK ? fmaf(q.m - all.m, tp.inv, log_s - logf(all.s)) : 0.f,
+                entropy = fmaf(q.w / q.s, -LN2F, log_s);
+    return {logprob > 0.f ? 0.f : logprob, logZ > 0.f ? 0.f : logZ, entropy < 0.f ? 0.f : entropy};   // (what rounding brings over the line)
 }
 template <bool MASK> __device__ __forceinline__ RowValues row_values(const Sums &all, const Sums &q, float x, const Temper &tp) {
     return row_values<MASK>(all, q, x, tp, logf(q.s));
@@ -446,9 +450,9 @@ template <bool SPLIT> __device__ __forceinline__ Split part_of(unsigned at_place
 }
 // Workgroup `group` of `groups` takes the place() -th piece of work.  Neighbouring workgroups start on the chip's eight dies in turn; a batch
 // often has a period (a query's candidates, a sequence's positions), and rows of one kind, those near the root with long work on their
-// masks, would all meet on one die.  So each die has a
-// stretch of its own, and each round of its compute units starts at another place.  (Scores under masks, every
-// eighth row near the root, us in turn / so: 1,024 rows at V = 256k bf16 96.7 / 92.9 with four wavefronts, 4,096 at V = 32k 53.1 / 49.2.)
+// masks, would all meet on one die.  So each die has a stretch of its own, and each round of its compute units starts at another place.
+// (Scores under masks, every eighth row near the root, us in turn / so: 1,024 rows at V = 256k bf16 96.7 / 92.9 with four wavefronts, 4,096
+// at V = 32k 53.1 / 49.2.)
 constexpr unsigned DIES = 8, DIE_UNITS = 32;
 __device__ __forceinline__ unsigned place(unsigned group, unsigned groups) {
     const unsigned die = group % DIES, each = groups / DIES, more = groups % DIES, mine = each + (die < more ? 1u : 0u);
@@ -457,6 +461,7 @@ __device__ __forceinline__ unsigned place(unsigned group, unsigned groups) {
     if ((round + 1u) * DIE_UNITS <= mine) i = round * DIE_UNITS + (i + 5u * round) % DIE_UNITS;
     return die * each + min(die, more) + i;
 }
+
 // ------------------------------------------------------------------------------------------
 // Forward.  ONE: rows of one tile, a wavefront each; else a workgroup has a row, or (SPLIT) 1 << shift of them have.
 template <typename T, bool MASK, bool W, bool ONE, bool SPLIT>
@@ -795,8 +800,9 @@ __device__ __forceinline__ void each_candidate(const Row &row, const uint32_t *m
         }
     }
 }
-// The k largest keys of a row, or of the tiles first, first + of, ... of it, into sh.list, in any order; sh.n: how many there are.  Digit by digit from the top: how many candidates
-// have each value of the digit below the digits settled so far, and in which of them the k-th largest lies.  By all wavefronts.
+// The k largest keys of a row, or of the tiles first, first + of, ... of it, into sh.list, in any order; sh.n: how many there are.  Digit by
+// digit from the top: how many candidates have each value of the digit below the digits settled so far, and in which of them the k-th
+// largest lies.  By all wavefronts.
 template <typename T, bool MASK>
 __device__ __forceinline__ void select_row(TopShared &sh, const Row &row, const uint32_t *mask, int V, int k, int first, int of, int wave, int nw, int lane) {
     const int tid = wave * WAVE + lane;

@@ -265,6 +265,9 @@ def odd_values(kind, B, V, rng):
         x[:, V // 4:V // 2] -= 250.0
         x[:, V // 2:] += 300.0
         x[:, 3 * V // 4:] += 60.0
+    elif kind == "stairs":              # a lane's tokens rise by no more than 30 at a time, by 240 in all; what is valid lies on the lowest stair, or below
+        x += 30.0 * (np.arange(V) * 9 // V)
+        x[:, ::3] -= 60.0 * (np.arange(V)[::3] < V // 9)
     elif kind == "low mass":            # the valid tokens far below the rest
         x[:, V // 2:] -= 300.0
     return x
@@ -272,7 +275,7 @@ def odd_values(kind, B, V, rng):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [100, 3001, 40000])
-@pytest.mark.parametrize("kind", ["filtered", "lowest", "high", "far", "ties", "peak", "rising", "falling", "low mass", "late peak"])
+@pytest.mark.parametrize("kind", ["filtered", "lowest", "high", "far", "ties", "peak", "rising", "falling", "low mass", "late peak", "stairs"])
 def test_odd_values(kind, V, dtype):
     rng = np.random.default_rng(V)
     B = 12
@@ -282,6 +285,8 @@ def test_odd_values(kind, V, dtype):
         valid[:, :V // 2] = False
     if kind == "late peak":
         valid[:, V // 2:] = False
+    if kind == "stairs":
+        valid[:, V // 9:] = False
     for v in (None, valid):
         tok = tokens_for(v, B, V, rng)
         c = Case(x, dtype, v, tok)
@@ -356,6 +361,61 @@ def test_rows_that_are_left_out_are_not_read():
         got = ids.cpu().numpy()
         assert ((got >= -1) & (got < V)).all()
         assert np.array_equal(got[rest], c.ref.top(128)[0][rest])
+
+
+def test_probabilities_are_not_above_one():
+    """One valid token, and all of them valid: log probabilities and log masses are 0 at most, entropies 0 at least."""
+    rng = np.random.default_rng(3)
+    B, V = 64, 5000
+    valid = np.zeros((B, V), bool)
+    tok = rng.integers(0, V, B)
+    valid[np.arange(B), tok] = True
+    valid[::2] = True
+    c = Case(rng.normal(0, 3, (B, V)), "f32", valid, tok, T=0.9)
+    lp, lz, h, _ = c.forward()
+    torch.cuda.synchronize()
+    assert (lp <= 0).all() and (lz <= 0).all() and (h >= 0).all()
+    assert (lp[1::2] >= -1e-6).all() and (h[1::2] <= 2e-5).all() and (lz[::2] >= -2e-5).all()
+
+
+def test_offsets_beyond_32_bits():
+    """Rows whose logits, masks and gradients lie beyond 2^32 bytes of their buffers' starts."""
+    B, V = 9_000, 262_144
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.empty((B, V), dtype=torch.bfloat16, device=DEV).normal_(0, 2, generator=g)
+    mask = torch.randint(-(1 << 31), (1 << 31) - 1, (B, V // 32), generator=g, device=DEV, dtype=torch.int32)
+    tokens = torch.randint(0, V, (B,), generator=g, device=DEV).to(torch.int32)
+    lp, lz, h, up = (torch.randn((B,), generator=g, device=DEV) for _ in range(4))
+    ids, lps = torch.zeros((B, 9), dtype=torch.int32, device=DEV), torch.zeros((B, 9), device=DEV)
+    rows = torch.tensor([0, 4_095, 4_096, 8_191, 8_192, 8_999], device=DEV)
+    kept, words, tk, g_up = x[rows].clone(), mask[rows].clone(), tokens[rows].clone(), up[rows].clone()
+    ppv.ppv_top_logprobs(x, 9, ids, lps, mask=mask)
+    ppv.ppv_token_logprobs_grad(x, tokens, x, lp, mask=mask, d_logprobs=up, logZ_valid=lz, entropy=h)      # in place
+    torch.cuda.synchronize()
+    ref = Scores(kept.double().cpu().numpy(), unpack(words.cpu().numpy(), V), tk.cpu().numpy(), 1.0)
+    check_values(lp[rows].cpu().numpy(), ref.logprobs, "logprobs")
+    check_values(lz[rows].cpu().numpy(), ref.logZ, "logZ_valid")
+    check_values(h[rows].cpu().numpy(), ref.entropy, "entropy")
+    want, size = ref.gradient(g_up.cpu().numpy(), None, None)
+    check_gradient(x[rows].float().cpu().numpy(), want, size, "bf16", "in place")
+    assert np.array_equal(ids[rows].cpu().numpy(), ref.top(9)[0])
+
+
+def test_two_streams_at_once():
+    """Split rows of calls that run at the same time on two streams."""
+    rng = np.random.default_rng(8)
+    cases = [Case(rng.normal(0, 2, (3, 128256)), "bf16", None, rng.integers(0, 128256, 3), seed=i) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = [[torch.zeros(3, device=DEV), torch.zeros((3, 5), dtype=torch.int32, device=DEV), torch.zeros((3, 5), device=DEV)] for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, s, (lp, ids, lps) in zip(cases, streams, outs):
+            ppv.ppv_token_logprobs(c.logits, c.tokens, lp, stream=s)
+            ppv.ppv_top_logprobs(c.logits, 5, ids, lps, stream=s)
+    torch.cuda.synchronize()
+    for c, (lp, ids, lps) in zip(cases, outs):
+        check_values(lp.cpu().numpy(), c.ref.logprobs, "logprobs")
+        assert np.array_equal(ids.cpu().numpy(), c.ref.top(5)[0])
 
 
 def test_gradient_against_differences():
