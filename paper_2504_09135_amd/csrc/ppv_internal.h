@@ -83,7 +83,9 @@ struct SplitRow {
     MarkedPair slice[PPV_LIST_MAX / 64];    // largest of 64 listed logits, the sum relative to it
     Marked list_e[PPV_LIST_MAX];
 };
+constexpr int PPV_STATS_WORDS = 8;          // what a call's first launch leaves of a row for its second one (ppv_token_logprobs_grad)
 struct SplitScratch {
+    float stats[PPV_SPLIT_MAX_ROWS][PPV_STATS_WORDS];
     uint32_t arrivals[PPV_SPLIT_MAX_ROWS];
     SplitRow row[PPV_SPLIT_MAX_ROWS];
 };
@@ -94,7 +96,7 @@ SplitScratch *ppv_split_scratch(hipStream_t stream, int rows);
 constexpr uint32_t PPV_LOOK_ONCE = 1u << 29;
 uint32_t ppv_split_mark(int split_shift);
 void ppv_split_look(bool again);
-// The area of eager calls on a stream, or constrained_sample_noalloc's array: its address, its size and where the rows' words begin,
+// The area of eager calls on a stream, or constrained_sample_noalloc's array: the address of its counts, its size from there on and where the rows' words begin,
 // for the tests that look at one or disturb it; look_again 0: calls from now on look once at a word.  (Exported, and not declared in
 // ppv.h.)
 extern "C" ppv_status ppv_split_area_for_tests(void *stream, int32_t fixed, int32_t look_again, void **area, int64_t *bytes, int64_t *words_at);

@@ -2275,9 +2275,10 @@ ppv_status ppv_split_area_for_tests(void *stream, int32_t fixed, int32_t look_ag
     }
     if (!p) return PPV_ENOMEM;
     ppv_split_look(look_again != 0);
-    *area = p;
-    *bytes = (int64_t)sizeof(SplitScratch);
-    *words_at = (int64_t)offsetof(SplitScratch, row);
+    constexpr size_t counts = offsetof(SplitScratch, arrivals);
+    *area = p->arrivals;
+    *bytes = (int64_t)(sizeof(SplitScratch) - counts);
+    *words_at = (int64_t)(offsetof(SplitScratch, row) - counts);
     return PPV_OK;
 }
 

@@ -8,6 +8,8 @@
 //   d_l            = d_logprob (1[v = t] - q) + d_logZ (q - p) - d_entropy q (log q + entropy),   d_logits = d_l / T
 // A row is read once, by all lanes of its wavefronts, each with its own running reference and sums relative to it; the lanes' sums are
 // brought to one reference at the end.  Sums are fp32: a lane adds at most 4,096 terms of one sign.
+#include <mutex>
+
 #include "ppv_rows.h"
 #include "ppv_split.h"
 
@@ -410,7 +412,6 @@ template <typename T> __device__ __forceinline__ float logit_of(const T *row, co
 
 struct Outputs {
     float *logprobs, *logZ_valid, *entropy, *stats;
-    Marked *words;   // the statistics for the library's own next launch, in the rows' scratch (see STATS_AT)
 };
 struct RowValues {
     float logprob, logZ, entropy;
@@ -425,18 +426,11 @@ template <bool MASK> __device__ __forceinline__ RowValues row_values(const Sums 
 template <bool MASK> __device__ __forceinline__ RowValues row_values(const Sums &all, const Sums &q, float x, const Temper &tp) {
     return row_values<MASK>(all, q, x, tp, logf(q.s));
 }
+static_assert(PPV_STATS_WORDS == PPV_LOGPROB_STATS, "one layout in both places");
 __device__ __forceinline__ void put_stats(float *stats, int64_t b, const Sums &all, const Sums &q, const RowValues &v) {
     float4 *at = (float4 *)(stats + b * PPV_LOGPROB_STATS);
     at[0] = {all.m, all.s, q.m, q.s};
     at[1] = {v.entropy, v.logprob, 0.f, 0.f};
-}
-// The words of a row's scratch that hold its statistics between two launches of one call, behind those of the parts: with the call's mark, so
-// that no later call takes one for a word of its own.
-constexpr int STATS_AT = PPV_SPLIT_MAX_PARTS * PART_WORDS, ROW_WORDS = (int)(sizeof(SplitRow) / sizeof(Marked));
-__device__ __forceinline__ void put_words(Marked *words, int64_t b, const Sums &all, const Sums &q, const RowValues &v, uint32_t mark) {
-    const float w[6] = {all.m, all.s, q.m, q.s, v.entropy, v.logprob};
-#pragma unroll
-    for (int i = 0; i < 6; i++) send(words + b * ROW_WORDS + STATS_AT + i, w[i], mark);
 }
 __device__ __forceinline__ void put_values(const Outputs &o, int64_t b, const RowValues &v) {
     if (o.logprobs) o.logprobs[b] = v.logprob;
@@ -513,7 +507,6 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
         const RowValues v = row_values<MASK>(r.all, r.q, x, tp);
         put_values(out, b, v);
         if (out.stats) put_stats(out.stats, b, r.all, r.q, v);
-        if (SPLIT && out.words) put_words(out.words, b, r.all, r.q, v, mark);
     }
 }
 
@@ -671,7 +664,7 @@ template <typename T, bool MASK, bool H, bool ONE>
 __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void gradient_kernel(const T *logits, int64_t row_stride, const int32_t *__restrict__ tokens,
                                                                                             const uint32_t *__restrict__ mask, int V, int n_words, int B, int shift,
                                                                                             T *d_logits, int64_t d_row_stride, const float *__restrict__ stats,
-                                                                                            int stats_stride, int stats_step, Upstream up, Temper tp) {
+                                                                                            Upstream up, Temper tp) {
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = blockDim.x / WAVE;
     const unsigned at_place = place(blockIdx.x, gridDim.x);
     const int64_t b = ONE ? (int64_t)at_place * SHORT_ROWS + wave : at_place >> shift;
@@ -688,9 +681,9 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void gra
     const Share share = share_of(tiles_in<T>(V), first, of);
     MaskedTile<T, MASK> tile;   // (asked for ahead of what the slopes are made of)
     tile.load(row, mrow, share.n > 0 ? share.at(0) : NO_TILE, lane, V);
-    const float *st = stats + b * stats_stride;   // (in the rows' scratch a word is a float and a mark)
-    const Sums all = {st[0], st[stats_step], 0.f}, q = {st[2 * stats_step], st[3 * stats_step], 0.f};
-    const Slope s = slope_of<T, MASK>(all, q, st[4 * stats_step], st[5 * stats_step], up, b, tok, tp);
+    const float *st = stats + b * PPV_LOGPROB_STATS;
+    const Sums all = {st[0], st[1], 0.f}, q = {st[2], st[3], 0.f};
+    const Slope s = slope_of<T, MASK>(all, q, st[4], st[5], up, b, tok, tp);
     if (s.nothing) put_zeros(to, first, of, lane, V);
     else put_tiles<T, MASK, H>(to, row, mrow, tile, s, tok, V, share, lane, tp.c);
 }
@@ -1328,7 +1321,7 @@ struct Rows {
     const int32_t *token_rows() const { return from_row(tokens, at); }
 };
 Outputs from_row(const Outputs &o, int64_t b) {
-    return {from_row(o.logprobs, b), from_row(o.logZ_valid, b), from_row(o.entropy, b), from_row(o.stats, b, PPV_LOGPROB_STATS), o.words};
+    return {from_row(o.logprobs, b), from_row(o.logZ_valid, b), from_row(o.entropy, b), from_row(o.stats, b, PPV_LOGPROB_STATS)};
 }
 Upstream from_row(const Upstream &u, int64_t b) { return {from_row(u.logprobs, b), from_row(u.logZ_valid, b), from_row(u.entropy, b)}; }
 // launch(rows) for all of a call's rows, MOST_ROWS at a time
@@ -1352,21 +1345,16 @@ template <typename T, bool MASK, bool W> void launch_score(const Rows &r, const 
     else PPV_SCORE(false, false);
 #undef PPV_SCORE
 }
-// Rows' statistics: `stride` floats from one row's to the next one's, `step` from word to word.
-struct Stats {
-    const float *at;
-    int stride, step;
-};
 template <typename T, bool MASK, bool H>
-void launch_gradient(const Rows &r, const Shape &sh, int shift, void *d_logits, int64_t d_stride, const Stats &stats, const Upstream &up, const Temper &tp) {
+void launch_gradient(const Rows &r, const Shape &sh, int shift, void *d_logits, int64_t d_stride, const float *stats, const Upstream &up, const Temper &tp) {
     const unsigned grid = sh.one ? sh.groups(r.n) : (unsigned)r.n << shift, block = sh.block;
     hipStream_t hs = r.stream;
     T *d = (T *)d_logits + r.at * d_stride;
-    const float *st = stats.at + r.at * stats.stride;
+    const float *st = from_row(stats, r.at, PPV_LOGPROB_STATS);
     if (sh.one)
-        PPV_LAUNCH((gradient_kernel<T, MASK, H, true>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, 0, d, d_stride, st, stats.stride, stats.step, from_row(up, r.at), tp);
+        PPV_LAUNCH((gradient_kernel<T, MASK, H, true>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, 0, d, d_stride, st, from_row(up, r.at), tp);
     else
-        PPV_LAUNCH((gradient_kernel<T, MASK, H, false>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, shift, d, d_stride, st, stats.stride, stats.step, from_row(up, r.at), tp);
+        PPV_LAUNCH((gradient_kernel<T, MASK, H, false>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, shift, d, d_stride, st, from_row(up, r.at), tp);
 }
 constexpr int MOST_HELD = 4;
 template <typename T, bool MASK, bool W>
@@ -1408,7 +1396,7 @@ ppv_status score_call(const Rows &rows, ppv_dtype dt, int B, const Area &area, c
 #undef PPV_CALL
     });
 }
-ppv_status gradient_call(const Rows &rows, ppv_dtype dt, int B, const Stats &stats, void *d_logits, int64_t d_stride, const Upstream &up, const Temper &tp) {
+ppv_status gradient_call(const Rows &rows, ppv_dtype dt, int B, const float *stats, void *d_logits, int64_t d_stride, const Upstream &up, const Temper &tp) {
     Shape sh = shape_of(rows.V, dt, B);
     // No wavefront waits for another here.  us with 4 / 8 / 16 wavefronts, bf16: V = 32k, 64 rows 4.7 / 4.9 / 6.6, 2,048 rows 51.5 / 49.5 / 46.7;
     // V = 128k, 16 rows 4.6 / 5.2 / 7.5, 1,024 rows 104.4 / 102.6 / 99.1; V = 50k fp32, 128 rows 11.6 / 12.1 / 12.2, 400 rows 36.6 / 35.0 / 35.5.
@@ -1434,7 +1422,7 @@ extern "C" ppv_status ppv_token_logprobs(const void *logits, ppv_dtype dt, int64
     const ppv_status st = check_row_args(logits, dt, row_stride, B, V, temperature, &tp);
     if (st != PPV_OK || B == 0) return st;
     if ((logprobs && !tokens) || (!logprobs && !logZ_valid && !entropy && !stats) || ((uintptr_t)stats & 15u) != 0) return PPV_EINVAL;
-    const Outputs out = {logprobs, logZ_valid, entropy, stats, nullptr};
+    const Outputs out = {logprobs, logZ_valid, entropy, stats};
     const Area area = area_for(V, dt, B, 0, PPV_SPLIT_MAX_PARTS, (hipStream_t)stream);
     return score_call({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, dt, B, area, out, entropy || stats, tp);
 }
@@ -1450,7 +1438,7 @@ extern "C" ppv_status ppv_token_logprobs_backward(const void *logits, ppv_dtype 
     st = check_gradient_args(logits, dt, row_stride, B, V, d_logits, d_row_stride);
     if (st != PPV_OK) return st;
     const Upstream up = {d_logprobs, d_logZ_valid, d_entropy};
-    return gradient_call({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, dt, B, {stats, PPV_LOGPROB_STATS, 1}, d_logits, d_row_stride, up, tp);
+    return gradient_call({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, dt, B, stats, d_logits, d_row_stride, up, tp);
 }
 
 extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, int64_t row_stride, const uint32_t *mask, const int32_t *tokens,
@@ -1463,8 +1451,12 @@ extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, 
     if ((logprobs || d_logprobs) && !tokens) return PPV_EINVAL;
     st = check_gradient_args(logits, dt, row_stride, B, V, d_logits, d_row_stride);
     if (st != PPV_OK) return st;
+    // (a row's workgroups each read what one of them would have written over)
+    for (const float *o : {logprobs, logZ_valid, entropy})
+        for (const float *u : {d_logprobs, d_logZ_valid, d_entropy})
+            if (o && u && (uintptr_t)o < (uintptr_t)(u + B) && (uintptr_t)u < (uintptr_t)(o + B)) return PPV_EINVAL;
     const Upstream up = {d_logprobs, d_logZ_valid, d_entropy};
-    Outputs out = {logprobs, logZ_valid, entropy, nullptr, nullptr};
+    Outputs out = {logprobs, logZ_valid, entropy, nullptr};
     const Rows rows = {0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream};
     Shape sh = shape_of(V, dt, B);
     const int nt = tiles_of(V, dt);
@@ -1477,17 +1469,19 @@ extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, 
     if (held > MOST_HELD || (mask && V >= 96000)) {
         const Area area = area_for(V, dt, B, 0, PPV_SPLIT_MAX_PARTS, (hipStream_t)stream);
         if (area.shift) {
-            out.words = (Marked *)area.scratch->row;
+            static std::mutex both;   // another thread's call on this stream does not come between the two launches
+            const std::lock_guard<std::mutex> lock(both);
+            out.stats = area.scratch->stats[0];
             st = score_call(rows, dt, B, area, out, entropy || d_entropy, tp);
             if (st != PPV_OK) return st;
-            return gradient_call(rows, dt, B, {(const float *)(out.words + STATS_AT), 2 * ROW_WORDS, 2}, d_logits, d_row_stride, up, tp);
+            return gradient_call(rows, dt, B, out.stats, d_logits, d_row_stride, up, tp);
         }
     }
     // Two or four workgroups to a row of a small batch.  (us with one / two / four, V = 32k bf16 masked: 32 rows 11.1 / 10.0 / 9.6, 64 rows 11.1 /
     // 10.2 / 10.3, 128 rows 11.3 / 10.9 / 17.6; without masks 7.8 / 7.2 / 7.1, 8.1 / 7.4 / 7.6, 8.1 / 8.1 / 13.0.)  They read the whole
     // row: not where another one writes it.
     int shift = 0;
-    while (!sh.one && held <= MOST_HELD && d_logits != logits && shift < 2 && nt >= 8 && (B << (shift + 1)) <= 128) shift++;
+    while (!sh.one && held <= MOST_HELD && d_logits != logits && shift < 2 && nt >= 8 && (int64_t)B << (shift + 1) <= 128) shift++;
     if (!sh.one) sh.block = (unsigned)nw * WAVE;
     return in_turns(rows, B, [&](const Rows &r) {
 #define PPV_CALL(T, MASK, W) launch_score_gradient<T, MASK, W>(r, sh, held, shift, d_logits, d_row_stride, out, up, tp)
@@ -1505,7 +1499,7 @@ extern "C" ppv_status ppv_top_logprobs(const void *logits, ppv_dtype dt, int64_t
     const ppv_status st = check_row_args(logits, dt, row_stride, B, V, temperature, &tp);
     if (st != PPV_OK || B == 0) return st;
     if (!top_ids || !top_logprobs || (logprobs && !tokens)) return PPV_EINVAL;
-    const Outputs out = {logprobs, nullptr, entropy, nullptr, nullptr};
+    const Outputs out = {logprobs, nullptr, entropy, nullptr};
     const Area area = area_for(V, dt, B, k, most_parts(k), (hipStream_t)stream);
     const int nt = (tiles_of(V, dt) + (1 << area.shift) - 1) >> area.shift, nw = waves_of(nt, (int64_t)B << area.shift, true), held = (nt + nw - 1) / nw;
     const unsigned block = (unsigned)nw * WAVE;

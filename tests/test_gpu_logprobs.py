@@ -1,5 +1,7 @@
 """ppv_token_logprobs, its gradient and ppv_top_logprobs against the plain 64-bit implementation, at the sizes, masks and values where
 they can go wrong."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -416,6 +418,42 @@ def test_two_streams_at_once():
     for c, (lp, ids, lps) in zip(cases, outs):
         check_values(lp.cpu().numpy(), c.ref.logprobs, "logprobs")
         assert np.array_equal(ids.cpu().numpy(), c.ref.top(5)[0])
+
+
+def test_threads_on_one_stream():
+    """Calls of two launches, whose second one reads what the first one left, from several threads on one stream, beside others there."""
+    rng = np.random.default_rng(12)
+    B, V, N = 4, 128256, 30
+    cases = [Case(rng.normal(0, 2, (B, V)), "bf16", rng.random((B, V)) < 0.3, rng.integers(0, V, B), seed=i) for i in range(3)]
+    up = torch.tensor([1.0, -0.5, 2.0, 0.25], device=DEV)
+    outs = [torch.zeros((N, B, V), dtype=torch.bfloat16, device=DEV) for _ in cases]
+    lps = [torch.zeros((N, B), device=DEV) for _ in cases]
+    ids, alternatives = torch.zeros((N, B, 20), dtype=torch.int32, device=DEV), torch.zeros((N, B, 20), device=DEV)
+    torch.cuda.synchronize()
+    stream, start = torch.cuda.Stream(), threading.Barrier(len(cases) + 1)
+
+    def gradients(c, out, lp):
+        start.wait()
+        for i in range(N):
+            ppv.ppv_token_logprobs_grad(c.logits, c.tokens, out[i], lp[i], mask=c.mask, d_logprobs=up, d_entropy=up, stream=stream)
+
+    def tops():
+        start.wait()
+        for i in range(N):
+            ppv.ppv_top_logprobs(cases[0].logits, 20, ids[i], alternatives[i], mask=cases[0].mask, stream=stream)
+    threads = [threading.Thread(target=gradients, args=a) for a in zip(cases, outs, lps)] + [threading.Thread(target=tops)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    g = up.cpu().numpy()
+    for c, out, lp in zip(cases, outs, lps):
+        check_values(lp[0].cpu().numpy(), c.ref.logprobs, "logprobs")
+        want, size = c.ref.gradient(g, None, g)
+        check_gradient(out[0].float().cpu().numpy(), want, size, "bf16", "threads")
+        assert (out == out[0]).all() and (lp == lp[0]).all()
+    assert np.array_equal(ids[0].cpu().numpy(), cases[0].ref.top(20)[0]) and (ids == ids[0]).all()
 
 
 def test_gradient_against_differences():

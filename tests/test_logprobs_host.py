@@ -44,6 +44,9 @@ def test_gradient_refusals(lib):
             assert call(**bad) == EINVAL, bad
         assert call(V=262145, stride=262152, d_stride=262152) == ERANGE
         assert call(B=0) == 0
+    # results over the upstream gradients that other workgroups of the row may still read
+    for lp in (NEVER, C.c_void_p(4096 + 12), C.c_void_p(4096 - 12)):
+        assert grad(g=NEVER, lp=lp) == EINVAL
     assert backward(st=None) == EINVAL and backward(st=C.c_void_p(4100)) == EINVAL
 
 
