@@ -17,8 +17,8 @@
  *     enqueue work on it and do not synchronise with the host.  Argument checks that need device
  *     data are not made; checks on host-visible arguments are.
  *   - An index is immutable after it is built; calls on different streams may run concurrently.
- *   - constrained_sample, ppv_sample_next, ppv_decode_step and ppv_decode_first_step spread the rows of a small batch over
- *     several workgroups, which meet in a scratch area.  Eager calls use one that belongs to their stream (7.5 MB; with
+ *   - constrained_sample, ppv_sample_next, ppv_decode_step, ppv_decode_first_step, ppv_token_logprobs, ppv_token_logprobs_grad and
+ *     ppv_top_logprobs spread the rows of a small batch over several workgroups, which meet in a scratch area.  Eager calls use one that belongs to their stream (7.5 MB; with
  *     hipStreamPerThread to the thread, for the first 64 threads that pass it), captured ones one that belongs to the capture
  *     (1.9 MB; up to 256 captures per GPU), so graphs may be replayed at the same time as one another and as eager calls, on any
  *     streams.  (One graph instantiated twice must not be replayed at the same time as itself.)  The first eager call that needs
@@ -344,8 +344,8 @@ ppv_status ppv_topm_mask(const ppv_index_t *index, const int32_t *prefixes, int3
  *   logZ_valid[b] = log sum_{v in mask} p_v (<= 0), as in constrained_sample; 0 without a mask.  logprobs + logZ_valid = log p_t, and their
  *                   sums over a member's tokens are log P_L(a) and log x(a) of Algorithm 1
  *   entropy[b]    = -sum_v q_v log q_v >= 0
- *   stats[b]      what ppv_token_logprobs_backward needs of the row, PPV_LOGPROB_STATS words: a logit m, sum_v exp(l_v - m / T); a logit
- *                 m' and the same over the valid tokens; the entropy; logprobs[b]; 0, 0
+ *   stats[b]      what ppv_token_logprobs_backward needs of the row, PPV_LOGPROB_STATS words: a number m near the largest logits,
+ *                 sum_v exp(l_v - m / T); m' and the same over the valid tokens; the entropy; logprobs[b]; 0, 0
  * A row without valid mass (an empty mask, or all valid tokens at -inf) has logZ_valid = -inf and entropy 0 (without a mask: a row
  * of -inf alone).  A row whose token is negative (-1, what the sampling calls give where no token could be drawn; padding) is left out: its
  * logits are not read and all its outputs are 0.
@@ -384,8 +384,8 @@ ppv_status ppv_token_logprobs_backward(const void *logits, ppv_dtype dt, int64_t
  * ppv_token_logprobs_grad -- ppv_token_logprobs and ppv_token_logprobs_backward in one call, for training whose upstream gradients are
  * known before the call (cross entropy: d_logprobs = -1 / rows; a policy gradient with given advantages): the row is read once where it
  * can be held on the chip, and no statistics are kept.  Same arguments, same results up to the rounding of sums taken in another order.
- *   logprobs, logZ_valid, entropy   float[B] or NULL (all may be)
- * Errors: as the two calls.
+ *   logprobs, logZ_valid, entropy   float[B] or NULL (all may be); not over d_logprobs, d_logZ_valid or d_entropy
+ * Errors: as the two calls; PPV_EINVAL also for results that overlap upstream gradients.
  */
 ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, int64_t row_stride, const uint32_t *mask, const int32_t *tokens,
                                    const float *d_logprobs, const float *d_logZ_valid, const float *d_entropy, int32_t B, int32_t V,
@@ -443,7 +443,7 @@ ppv_status ppv_disc_select(const float *logx, int32_t n_candidates, int32_t K, i
  * read once from the environment variable of the same name without the TUNE_ part (PPV_WAVES_PER_ROW, ...)
  * when the library is loaded; no per-step call reads the environment.  Setting one while calls are being
  * issued from another thread is a race.
- *   PPV_TUNE_WAVES_PER_ROW   wavefronts per row of the sampling kernels, 1..16; 0 = the library's table
+ *   PPV_TUNE_WAVES_PER_ROW   wavefronts per row of the sampling kernels and those of log probabilities, 1..16; 0 = the library's table
  *   PPV_TUNE_TOPM_WAVES      the same for ppv_topm_mask
  *   PPV_TUNE_TOPM_STREAMING  1: every row of ppv_topm_mask takes the whole-row select (tests); 2: the usual select,
  *                            but also for mask-only calls on prefixes with few children (no counting); 0 = as needed

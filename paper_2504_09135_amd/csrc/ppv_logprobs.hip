@@ -177,7 +177,7 @@ template <typename T> __device__ __forceinline__ uint32_t bits_at(const uint32_t
 template <typename T, bool PAD> __device__ __forceinline__ void unpack_group(const u32x4 &r, int left, float (&x)[Elem<T>::EPL]) {
     unpack_fresh<T>(r, x);
     if (PAD) {
-        asm volatile("" : "+v"(left));   // (compared here: ahead of the loop over rows each token's comparison takes two scalar registers)
+        asm volatile("" : "+v"(left));   // (compared here: ahead of the loop over tiles each token's comparison takes two scalar registers)
 #pragma unroll
         for (int k = 0; k < Elem<T>::EPL; k++) x[k] = k < left ? x[k] : -INFINITY;
     }
