@@ -883,11 +883,11 @@ __device__ __forceinline__ void top_tile_as(const MaskedTile<T, MASK> &mt, int i
         __builtin_amdgcn_sched_barrier(0);   // one group's tokens in registers at a time
     }
 }
-// A bound that at least k of the lanes' tokens `u` are not below: the k-th largest of them, or a little less.  1 where there are fewer.  By one
-// wavefront, bit by bit from the first in which they differ.
+// A bound that at least k of the lanes' tokens `u` are not below: the k-th largest of them, or a little less; where SPARE is given, any that no
+// more than k + SPARE are not below will do.  1 where there are fewer.  By one wavefront, bit by bit from the first in which they differ.
 constexpr int BOUND_BITS = 12;
 constexpr int FEW_ASKED = 20;   // up to so many candidates the bound is found from 64 tokens: a quarter more tokens reach it
-template <int N, int BITS = BOUND_BITS> __device__ __forceinline__ uint32_t bound_of(const uint32_t (&u)[N], int k) {
+template <int N, int BITS = BOUND_BITS, int SPARE = 0> __device__ __forceinline__ uint32_t bound_of(const uint32_t (&u)[N], int k) {
     uint32_t hi = 0u, lo = 0u;   // the largest, and the complement of the smallest that is one
     int some = 0;
 #pragma unroll
@@ -908,7 +908,7 @@ template <int N, int BITS = BOUND_BITS> __device__ __forceinline__ uint32_t boun
 #pragma unroll
         for (int i = 0; i < N; i++) n += __popcll(__ballot(u[i] >= try_at));
         if (n >= k) t = try_at;
-        if (n == k) break;
+        if (n >= k && n <= k + SPARE) break;
     }
     return t > 1u ? t : 1u;
 }
@@ -937,12 +937,14 @@ __device__ __forceinline__ void list_group(TopShared &sh, const u32x4 &raw, uint
         } while (m);
     }
 }
-// Takes those of the n listed keys out that are not among the first k, but for ties of the last one's logit.  By one wavefront, in place.
+// Takes those of the n listed keys out that are not among the first k, but for a few and for ties of the last one's logit.  By one wavefront, in
+// place.
+constexpr int SPARE = 48, FEW_MORE = 12, MOST_ALIKE = 256;
 template <int N> __device__ __forceinline__ int thin_out(TopShared &sh, int n, int k, int lane) {
     uint32_t u[N];
 #pragma unroll
     for (int i = 0; i < N; i++) u[i] = i * WAVE + lane < n ? (uint32_t)(sh.list[i * WAVE + lane] >> TOKEN_BITS) : 0u;
-    const uint32_t bound = bound_of<N, 32>(u, k);
+    const uint32_t bound = bound_of<N, 32, FEW_MORE>(u, k);
     int kept = 0;
 #pragma unroll 1
     for (int i = 0; i * WAVE < n; i++) {
@@ -955,7 +957,6 @@ template <int N> __device__ __forceinline__ int thin_out(TopShared &sh, int n, i
     return kept;
 }
 // The same where it pays (placing n keys takes n^2 comparisons), by all wavefronts, with a barrier ahead; -1: more than `most` ties are left.
-constexpr int SPARE = 48, MOST_ALIKE = 256;
 __device__ __forceinline__ int thinned_out(TopShared &sh, int n, int k, int most, int wave, int lane) {
     if (n <= k + SPARE) return n;
     if (wave == 0) {
@@ -967,15 +968,30 @@ __device__ __forceinline__ int thinned_out(TopShared &sh, int n, int k, int most
 }
 // The row's first k of n listed keys, by all wavefronts: f(place, key) for each of them, in no order.  A key's place is how many are larger:
 // a wavefront has every nw-th key, one to a lane, and counts for one after the other in as many comparisons as there are 64 keys; or, one or
-// two wavefronts, each lane counts for its own.
+// two wavefronts, each lane counts for its own, two at a time where there are more.  (73 of 364 bf16 tokens, 5,640 rows, one at a time 38.8 us,
+// so 30.1, with the earlier end of the bound's search.)
 template <typename F> __device__ __forceinline__ void each_place(const TopShared &sh, int n, int k, int wave, int nw, int lane, F f) {
-    if (nw <= 2) {
-        for (int i = wave * WAVE + lane; i < n; i += nw * WAVE) {
-            const uint64_t key = sh.list[i];
-            int place = 0;
+    if (n <= nw * WAVE && nw <= 2) {
+        const uint64_t key = wave * WAVE + lane < n ? sh.list[wave * WAVE + lane] : 0ull;
+        int place = 0;
 #pragma unroll 8
-            for (int j = 0; j < n; j++) place += sh.list[j] > key;
+        for (int j = 0; j < n; j++) place += sh.list[j] > key;
+        if (place < k && key) f(place, key);
+        return;
+    }
+    if (nw <= 2) {
+        for (int i = wave * WAVE + lane; i - lane < n; i += 2 * nw * WAVE) {   // (two keys a lane)
+            const int i2 = i + nw * WAVE;
+            const uint64_t key = i < n ? sh.list[i] : 0ull, key2 = i2 < n ? sh.list[i2] : 0ull;
+            int place = 0, place2 = 0;
+#pragma unroll 8
+            for (int j = 0; j < n; j++) {
+                const uint64_t other = sh.list[j];
+                place += other > key;
+                place2 += other > key2;
+            }
             if (place < k && key) f(place, key);
+            if (place2 < k && key2) f(place2, key2);
         }
         return;
     }
@@ -1121,7 +1137,18 @@ __global__ __launch_bounds__(MOST_WAVES *WAVE) void top_kernel(const T *__restri
         // lanes with more than one such group: all of theirs are looked at again, one lane's by the whole wavefront or each its own
         if (__popcll(lanes) * ((share.n * 4 + WAVE - 1) / WAVE) > share.n * 4) {
             if (more)
-                for (int i = 0; i < share.n * 4; i++) look(i, lane);
+                for (int i = 0; i < share.n * 4; i += 4) {   // (a tile's groups, asked for at once)
+                    u32x4 raw[4];
+                    uint32_t bits[4];
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const int v = token_of(i + j, lane);
+                        raw[j] = __builtin_amdgcn_raw_buffer_load_b128(row.buf, (uint32_t)v * (uint32_t)sizeof(T), 0, 0);
+                        bits[j] = MASK ? bits_at<T>(mrow, v, V) : 0xFFu;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; j++) list_group<T>(sh, raw[j], bits[j], token_of(i + j, lane), V, least);
+                }
         } else {
             for (uint64_t rest = lanes; rest; rest &= rest - 1ull)
                 for (int i = lane; i < share.n * 4; i += WAVE) look(i, __ffsll((long long)rest) - 1);
@@ -1214,10 +1241,10 @@ int tiles_of(int V, ppv_dtype dt) {
 // through with all of them; each wavefront takes part in what follows the pass over a row.  us with 1 / 2 / 4 / 8 / 16: scores under
 // prefixes' masks, bf16, V = 8k, 300 rows 8.9 / 7.3 / 5.9 / 5.8, 4,000 rows 19.8 / 18.8 / 19.4; V = 32k, 4,096 rows 54.7 (two) / 49.2 / 55.6 / 100;
 // V = 256k, 1,024 rows 92.9 (four) / 92.7 / 107; fp32, V = 2,100 (three tiles), 4,000 rows 12.6 / 13.1 / 15.8.  Alternatives, V = 3,224 bf16,
-// 4,000 rows 12.6 / 13.4; V = 8k 18.6 / 19.0 / 21.4; 300 rows 9.4 / 8.0 / 7.1 / 7.0.
-int waves_of(int nt, int64_t rows, bool top = false) {
+// 4,000 rows 12.6 / 13.4, but 128 of them of V = 2,932, 3,408 rows 84.8 / 33.1; V = 8k 18.6 / 19.0 / 21.4; 300 rows 9.4 / 8.0 / 7.1 / 7.0.
+int waves_of(int nt, int64_t rows, int k = 0) {   // k: alternatives; more than 64 of them are not bounded well by one wavefront's 128 maxima
     int cap = rows <= 256 ? 16 : (nt >= 48 || rows <= 512 ? 8 : 4);
-    if (rows >= 2048 && nt <= 4) cap = nt <= 3 ? 1 : (top ? 2 : 4);
+    if (rows >= 2048 && nt <= 4) cap = nt <= 3 && k <= WAVE ? 1 : (k ? 2 : 4);
     if (const int v = ppv_tuning(PPV_TUNE_WAVES_PER_ROW)) cap = v;
     int nw = 1;
     while (nw < nt && nw * 2 <= cap) nw <<= 1;
@@ -1501,7 +1528,7 @@ extern "C" ppv_status ppv_top_logprobs(const void *logits, ppv_dtype dt, int64_t
     if (!top_ids || !top_logprobs || (logprobs && !tokens)) return PPV_EINVAL;
     const Outputs out = {logprobs, nullptr, entropy, nullptr};
     const Area area = area_for(V, dt, B, k, most_parts(k), (hipStream_t)stream);
-    const int nt = (tiles_of(V, dt) + (1 << area.shift) - 1) >> area.shift, nw = waves_of(nt, (int64_t)B << area.shift, true), held = (nt + nw - 1) / nw;
+    const int nt = (tiles_of(V, dt) + (1 << area.shift) - 1) >> area.shift, nw = waves_of(nt, (int64_t)B << area.shift, k), held = (nt + nw - 1) / nw;
     const unsigned block = (unsigned)nw * WAVE;
     return in_turns({0, 0, V, (V + 31) / 32, row_stride, logits, mask, tokens, (hipStream_t)stream}, B, [&](const Rows &r) {
 #define PPV_CALL(T, MASK, W) launch_top<T, MASK, W>(r, block, held, area, k, top_ids, top_logprobs, out, tp)

@@ -163,6 +163,20 @@ def test_many_rows(B, V, dtype):
     Case(x, dtype, valid, tokens_for(valid, B, V, rng)).check_all((20,))
 
 
+@pytest.mark.parametrize("V,dtype", [(40, "f32"), (364, "bf16"), (1024, "f32"), (2932, "bf16"), (5000, "bf16")])
+def test_many_alternatives_of_short_rows(V, dtype):
+    """A wavefront or two to a row, and nearly as many alternatives as there are maxima to bound them with, or more than tokens."""
+    rng = np.random.default_rng(V)
+    B = 2100
+    x = rng.normal(0, 2, (B, V))
+    x[::3] = np.round(x[::3])       # many equal ones
+    valid = rng.random((B, V)) < rng.choice([0.02, 0.5, 1.0], (B, 1))
+    for v in (None, valid):
+        c = Case(x, dtype, v, rng.integers(0, V, B))
+        for k in (40, 64, 65, 73, 100, 128):
+            c.check_top(k)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T", [0.05, 0.6, 1.0, 1.7, 30.0])
 def test_temperatures(T, dtype):
