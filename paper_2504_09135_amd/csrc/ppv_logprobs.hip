@@ -648,11 +648,11 @@ template <typename T> __device__ __forceinline__ void put_zeros(T *out, int firs
 #pragma unroll
         for (int j = 0; j < 4; j++) put_group(out, t * G::TILE + j * G::PER_LOAD + lane * G::EPL, V, d);
 }
-// The wavefront's tiles, the first of them asked for; each is read before another one is written: out may be the logits themselves.
+// The wavefront's tiles from the i-th on, which is asked for; each is read before another one is written: out may be the logits themselves.
 template <typename T, bool MASK, bool H>
-__device__ __forceinline__ void put_tiles(T *out, const Row &row, const uint32_t *mask, MaskedTile<T, MASK> &now, const Slope &s, int tok, int V, const Share &share, int lane, float c) {
+__device__ __forceinline__ void put_tiles(T *out, const Row &row, const uint32_t *mask, MaskedTile<T, MASK> &now, const Slope &s, int tok, int V, const Share &share, int i, int lane, float c) {
     MaskedTile<T, MASK> next;
-    for (int i = 0; i < share.n; i++) {
+    for (; i < share.n; i++) {
         next.load(row, mask, i + 1 < share.n ? share.at(i + 1) : NO_TILE, lane, V);
         now.settle(share.at(i), lane, V);
         put_tile<T, MASK, H>(out, now, s, share.at(i), lane, tok, V, c);
@@ -685,12 +685,12 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void gra
     const Sums all = {st[0], st[1], 0.f}, q = {st[2], st[3], 0.f};
     const Slope s = slope_of<T, MASK>(all, q, st[4], st[5], up, b, tok, tp);
     if (s.nothing) put_zeros(to, first, of, lane, V);
-    else put_tiles<T, MASK, H>(to, row, mrow, tile, s, tok, V, share, lane, tp.c);
+    else put_tiles<T, MASK, H>(to, row, mrow, tile, s, tok, V, share, 0, lane, tp.c);
 }
 
-// Both: the sums, then the gradient.  A wavefront holds its tiles, at most HELD; HELD = 0: they are read again.  1 << shift workgroups may
-// have a row: each takes all of its sums, which needs no word from another, and its part of the gradient.
-template <typename T, bool MASK, bool W, bool ONE, int HELD>
+// Both: the sums, then the gradient.  A wavefront holds its first HELD tiles; MORE: it may have others, which are read again.  1 << shift
+// workgroups may have a row: each takes all of its sums, which needs no word from another, and its part of the gradient.
+template <typename T, bool MASK, bool W, bool ONE, int HELD, bool MORE>
 __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void score_gradient_kernel(const T *logits, int64_t row_stride, const int32_t *__restrict__ tokens,
                                                                                                   const uint32_t *__restrict__ mask, int V, int n_words, int B, int shift,
                                                                                                   T *d_logits, int64_t d_row_stride, Outputs out, Upstream up, Temper tp) {
@@ -711,7 +711,7 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
     const Row row = row_of(at, V);
     const uint32_t *mrow = MASK ? mask + b * n_words : nullptr;
     const Share share = share_of(tiles_in<T>(V), wave, nw);
-    MaskedTile<T, MASK> held[HELD ? HELD : 1];
+    MaskedTile<T, MASK> held[HELD];
 #pragma unroll
     for (int i = 0; i < HELD; i++) held[i].load(row, mrow, i < share.n ? share.at(i) : NO_TILE, lane, V);
     float x = wave == 0 ? logit_of(at, mrow, tok, V) : 0.f;
@@ -723,7 +723,7 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
             held[i].settle(share.at(i), lane, V);
             take_tile<T, MASK, W>(row, held[i], share.at(i), V, lane, tp.c, step, a);
         }
-    if (HELD == 0) take_tiles<T, MASK, W>(row, mrow, V, share, 0, lane, tp.c, step, a);
+    if (MORE) take_tiles<T, MASK, W>(row, mrow, V, share, HELD, lane, tp.c, step, a);
     const Part p = workgroup_part<MASK, W, ONE>(sh, a, x, wave, nw, lane);
     const RowSums r = row_sums<T, MASK, ONE>(sh, row, mrow, V, p, wave, nw, lane, tp.c);
     const RowValues v = row_values<MASK>(r.all, r.q, x, tp);
@@ -736,9 +736,10 @@ __global__ __launch_bounds__(ONE ? SHORT_ROWS *WAVE : MOST_WAVES *WAVE) void sco
 #pragma unroll
     for (int i = 0; i < HELD; i++)   // (four neighbouring wavefronts' tiles are one part's: those of the four SIMDs)
         if (i < share.n && (ONE || ((share.at(i) >> 2) & ((1 << shift) - 1)) == part)) put_tile<T, MASK, W>(to, held[i], s, share.at(i), lane, tok, V, tp.c);
-    if (HELD == 0) {
-        held[0].load(row, mrow, share.n > 0 ? share.at(0) : NO_TILE, lane, V);
-        put_tiles<T, MASK, W>(to, row, mrow, held[0], s, tok, V, share, lane, tp.c);
+    if (MORE) {
+        MaskedTile<T, MASK> &tile = held[0];
+        tile.load(row, mrow, HELD < share.n ? share.at(HELD) : NO_TILE, lane, V);
+        put_tiles<T, MASK, W>(to, row, mrow, tile, s, tok, V, share, HELD, lane, tp.c);
     }
 }
 
@@ -1383,20 +1384,23 @@ void launch_gradient(const Rows &r, const Shape &sh, int shift, void *d_logits, 
     else
         PPV_LAUNCH((gradient_kernel<T, MASK, H, false>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, r.n, shift, d, d_stride, st, from_row(up, r.at), tp);
 }
+// The tiles a wavefront holds of rows that it cannot hold whole: what is held is not read again, under masks four would not leave the registers
+// that the sums take.  (us with none / two / three / four held by each of sixteen wavefronts, 600 rows: V = 100k fp32 134 / 124 / 115 / 108, masked
+// 146 / 132 / 132, V = 160k 222 / 208 / 200 / 192, masked 231 / 216 / 220; 1,024 rows at V = 256k bf16 292 / 271 / 259 / 245, masked 304 / 280 / 289.)
 constexpr int MOST_HELD = 4;
 template <typename T, bool MASK, bool W>
 void launch_score_gradient(const Rows &r, const Shape &sh, int held, int shift, void *d_logits, int64_t d_stride, const Outputs &out, const Upstream &up, const Temper &tp) {
     const unsigned grid = sh.groups(r.n) << shift, block = sh.block;
     hipStream_t hs = r.stream;
     T *d = (T *)d_logits + r.at * d_stride;
-#define PPV_SCORE_GRADIENT(ONE, HELD)                                                                                                   \
-    PPV_LAUNCH((score_gradient_kernel<T, MASK, W, ONE, HELD>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, \
+#define PPV_SCORE_GRADIENT(ONE, HELD, MORE)                                                                                                 \
+    PPV_LAUNCH((score_gradient_kernel<T, MASK, W, ONE, HELD, MORE>), r.logits_as<T>(), r.stride, r.token_rows(), r.mask_rows(), r.V, r.n_words, \
                r.n, shift, d, d_stride, from_row(out, r.at), from_row(up, r.at), tp)
-    if (sh.one) PPV_SCORE_GRADIENT(true, 1);
-    else if (held > MOST_HELD) PPV_SCORE_GRADIENT(false, 0);
-    else if (held > 2) PPV_SCORE_GRADIENT(false, 4);
-    else if (held > 1) PPV_SCORE_GRADIENT(false, 2);
-    else PPV_SCORE_GRADIENT(false, 1);
+    if (sh.one) PPV_SCORE_GRADIENT(true, 1, false);
+    else if (held > MOST_HELD) PPV_SCORE_GRADIENT(false, (MASK ? 2 : MOST_HELD), true);
+    else if (held > 2) PPV_SCORE_GRADIENT(false, 4, false);
+    else if (held > 1) PPV_SCORE_GRADIENT(false, 2, false);
+    else PPV_SCORE_GRADIENT(false, 1, false);
 #undef PPV_SCORE_GRADIENT
 }
 template <typename T, bool MASK, bool W>

@@ -352,6 +352,26 @@ def test_gradient_in_place(V, dtype):
         c.check_gradient(c.buf, c.up, how + " in place")
 
 
+@pytest.mark.parametrize("split", [0, 1])
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("V,dtype", [(66_000, "f32"), (100_003, "f32"), (140_001, "bf16"), (262_144, "bf16")])
+def test_rows_that_no_workgroup_holds(V, dtype, masked, split):
+    """Parts of a row that are read again for the gradient, which may lie over it."""
+    rng = np.random.default_rng(V)
+    B = 7
+    x = rng.normal(0, 2, (B, V))
+    valid = hand_made_masks(B, V, rng) if masked else None
+    with tuning(ppv.PPV_TUNE_ROW_SPLIT, split):
+        c = Case(x, dtype, valid, tokens_for(valid, B, V, rng), T=0.9)
+        c.check_all((3,))
+        dev = {n: to_dev(v) for n, v in c.up.items()}
+        lp = torch.zeros(B, device=DEV)
+        ppv.ppv_token_logprobs_grad(c.logits, c.tokens, c.logits, lp, mask=c.mask, temperature=c.T, **dev)
+        torch.cuda.synchronize()
+        check_values(lp.cpu().numpy(), c.ref.logprobs, "in place")
+        c.check_gradient(c.buf, c.up, "in place")
+
+
 def test_rows_that_are_left_out_are_not_read():
     """A row of NaN whose token is negative leaves zeros; NaN in one row does not reach another."""
     rng = np.random.default_rng(2)
