@@ -1495,8 +1495,9 @@ extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, 
     while (!sh.one && nw < MOST_WAVES && nt > MOST_HELD * nw) nw *= 2;   // enough wavefronts to hold the row, if there are as many
     const int held = (nt + nw - 1) / nw;
     // Few rows that no workgroup can hold, or not without long work on their masks: the sums by several workgroups, then the gradient.  (us
-    // in one launch / in two, 32 rows: V = 100k fp32 25.0 / 17.3, masked 31.9 / 19.1; V = 128k bf16 masked 29.4 / 18.7, but without a mask
-    // 16.2 / 16.2 and V = 64k masked 14.5 / 14.2, V = 50k fp32 masked 15.6 / 16.3.)
+    // in one launch / in two: V = 100k fp32 32 rows 20.9 / 12.1, 128 rows 28.4 / 31.5, masked 30.1 / 13.8, 36.5 / 34.4; V = 256k bf16 36.7 / 14.1,
+    // 43.1 / 40.0; V = 100k bf16 masked 20.6 / 12.6, 25.8 / 24.2, but 32 rows without a mask, V = 128k 16.2 / 16.2, and masked, V = 64k 14.5 / 14.2,
+    // V = 50k fp32 15.6 / 16.3.)
     if (held > MOST_HELD || (mask && V >= 96000)) {
         const Area area = area_for(V, dt, B, 0, PPV_SPLIT_MAX_PARTS, (hipStream_t)stream);
         if (area.shift) {
