@@ -150,10 +150,11 @@ template <bool W> __device__ __forceinline__ Run both(const Run &a, const Run &b
     const float da = most(ra - R, FAINT), db = most(rb - R, FAINT), fa = fast_exp2(da), fb = fast_exp2(db);
     return {R, fa * a.s + fb * b.s, W ? fa * fmaf(da, a.s, a.w) + fb * fmaf(db, b.s, b.w) : 0.f};
 }
-// relative to a logit that makes the sum about 1: weights are then no smaller against it than they are
+// relative to a logit that makes the sum about 1: weights are then no smaller against it than they are.  (Any number will do.  At temperatures
+// near fp32's largest numbers that logit is outside them, or 1 / c infinite: the largest number, against which the sum is V at most.)
 __device__ __forceinline__ Sums sums_of(const Run &a, float c) {
     if (!(a.s != 0.f)) return no_sums();
-    const float m = (a.r + fast_log2(a.s)) * __builtin_amdgcn_rcpf(c), d = fmaf(-m, c, a.r), f = fast_exp2(d);
+    const float m = most(fminf((a.r + fast_log2(a.s)) * __builtin_amdgcn_rcpf(c), -LOWEST), LOWEST), d = fmaf(-m, c, a.r), f = fast_exp2(d);
     return {m, f * a.s, f * fmaf(d, a.s, a.w)};
 }
 
@@ -416,10 +417,12 @@ struct Outputs {
 struct RowValues {
     float logprob, logZ, entropy;
 };
+// (a - b) / T + more; the difference may be outside fp32 where this is not
+__device__ __forceinline__ float over_t(float a, float b, const Temper &tp, float more) { return 2.f * fmaf(0.5f * a - 0.5f * b, tp.inv, 0.5f * more); }
 // what the sums say.  Without mass (no valid token, or all at -inf): -inf, and an entropy of 0.
 template <bool MASK> __device__ __forceinline__ RowValues row_values(const Sums &all, const Sums &q, float x, const Temper &tp, float log_s) {
     if (!(q.s != 0.f)) return {-INFINITY, -INFINITY, 0.f};
-    const float logprob = (x - q.m) * tp.inv - log_s, logZ = MASK ? fmaf(q.m - all.m, tp.inv, log_s - logf(all.s)) : 0.f,
+    const float logprob = over_t(x, q.m, tp, -log_s), logZ = MASK ? over_t(q.m, all.m, tp, log_s - logf(all.s)) : 0.f,
                 entropy = fmaf(q.w / q.s, -LN2F, log_s);
     return {logprob > 0.f ? 0.f : logprob, logZ > 0.f ? 0.f : logZ, entropy < 0.f ? 0.f : entropy};   // (what rounding brings over the line)
 }
@@ -531,12 +534,12 @@ template <typename T, bool MASK> __device__ __forceinline__ Slope slope_of(const
     Slope s;
     const float g = up.logprobs && logprob > -INFINITY ? up.logprobs[b] : 0.f;   // (a log probability of -inf has no slope)
     const float z = MASK && up.logZ_valid ? up.logZ_valid[b] : 0.f, h = up.entropy ? up.entropy[b] : 0.f;
-    const float over = tp.inv / q.s, c = tp.c;
+    const float over = 1.f / q.s, c = tp.c;   // (1 / T last: it may be one of fp32's subnormal numbers)
     s.nothing = __builtin_amdgcn_readfirstlane(tok < 0 || !(q.s != 0.f));
     s.far = __builtin_amdgcn_readfirstlane(!(fabsf(q.m * c) < FAR_OFF && fabsf(all.m * c) < FAR_OFF));
-    s.a = over * (z - g - h * (entropy - logf(q.s)));
-    s.b = over * (-LN2F * h);
-    s.z = MASK && z != 0.f ? z * tp.inv / all.s : 0.f;
+    s.a = over * (z - g - h * (entropy - logf(q.s))) * tp.inv;
+    s.b = over * (-LN2F * h) * tp.inv;
+    s.z = MASK && z != 0.f ? z / all.s * tp.inv : 0.f;
     s.r = q.m;
     s.rp = all.m;
     s.together = false;
