@@ -523,7 +523,9 @@ struct Upstream {
 //              enough against all: their exponents are as far below 0 then, and rounded as much more coarsely (2^-24 off for 2^-24 of the
 //              weight is 1e-6, nothing to a gradient in bf16 but more than one in fp32 is rounded by: 2^-4)
 //   else       y and e relative to the valid tokens' reference r, e_p = 2^(x c - rp)
-// In rows beyond FAR_OFF, r and rp are logits, and y = (x - r) c.
+// In rows beyond FAR_OFF, r and rp are logits, and y = (x - r) c.  So are they where b FAINT may be infinite, at temperatures below 1e-35: e is
+// multiplied by y first then, which is 0 where e is.
+constexpr float STEEP = 1e35f;
 template <typename T> constexpr float TOGETHER_MOST = sizeof(T) == 4 ? 4.f : 24.f;
 struct Slope {
     float r, a, b, rp, z, at_token;
@@ -536,10 +538,10 @@ template <typename T, bool MASK> __device__ __forceinline__ Slope slope_of(const
     const float z = MASK && up.logZ_valid ? up.logZ_valid[b] : 0.f, h = up.entropy ? up.entropy[b] : 0.f;
     const float over = 1.f / q.s, c = tp.c;   // (1 / T last: it may be one of fp32's subnormal numbers)
     s.nothing = __builtin_amdgcn_readfirstlane(tok < 0 || !(q.s != 0.f));
-    s.far = __builtin_amdgcn_readfirstlane(!(fabsf(q.m * c) < FAR_OFF && fabsf(all.m * c) < FAR_OFF));
     s.a = over * (z - g - h * (entropy - logf(q.s))) * tp.inv;
     s.b = over * (-LN2F * h) * tp.inv;
     s.z = MASK && z != 0.f ? z / all.s * tp.inv : 0.f;
+    s.far = __builtin_amdgcn_readfirstlane(!(fabsf(q.m * c) < FAR_OFF && fabsf(all.m * c) < FAR_OFF && fabsf(s.b) < STEEP));
     s.r = q.m;
     s.rp = all.m;
     s.together = false;
@@ -621,7 +623,7 @@ __device__ __forceinline__ void put_tile_as(T *out, const MaskedTile<T, MASK> &m
 #pragma unroll
                 for (int k = 0; k < G::EPL; k++) {
                     const float y = exponent<FAR>(x[k], s.r, c), e = fast_exp2(y);
-                    d[k] = e * (H ? fmaf(s.b, most(y, FAINT), s.a) : s.a);
+                    d[k] = !H ? e * s.a : FAR ? fmaf(e * most(y, FAINT), s.b, e * s.a) : e * fmaf(s.b, most(y, FAINT), s.a);
                     if (MASK) d[k] = __uint_as_float(__float_as_uint(d[k]) & all_ones_if(bits, k));
                 }
             }

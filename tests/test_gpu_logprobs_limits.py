@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [100, 3001, 40000])
-@pytest.mark.parametrize("T", [3.0e38, 1.0e38, 5.0e37, 1.0e-30])
+@pytest.mark.parametrize("T", [3.0e38, 1.0e38, 5.0e37, 1.0e-30, 1.0e-37])
 def test_largest_and_smallest_temperatures(T, V, dtype):
     """log2(e) / T and 1 / T from fp32's subnormal numbers (which round to 2^-22 of their size at T = 3e38) to near its largest.  Where T
     is large the distribution is even, whatever the logits, and T times a log probability may be outside fp32.  The upstream gradients are
