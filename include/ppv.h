@@ -346,6 +346,8 @@ ppv_status ppv_topm_mask(const ppv_index_t *index, const int32_t *prefixes, int3
  *   entropy[b]    = -sum_v q_v log q_v >= 0
  *   stats[b]      what ppv_token_logprobs_backward needs of the row, PPV_LOGPROB_STATS words: a number m near the largest logits,
  *                 sum_v exp(l_v - m / T); m' and the same over the valid tokens; the entropy; logprobs[b]; 0, 0
+ * NaN or +inf at tokens that are not valid counts for logZ_valid alone, which is NaN then; logprobs, the entropy, their gradients and the
+ * alternatives of ppv_top_logprobs are what they are without it.
  * A row without valid mass (an empty mask, or all valid tokens at -inf) has logZ_valid = -inf and entropy 0 (without a mask: a row
  * of -inf alone).  A row whose token is negative (-1, what the sampling calls give where no token could be drawn; padding) is left out: its
  * logits are not read and all its outputs are 0.

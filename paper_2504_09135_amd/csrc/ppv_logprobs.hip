@@ -383,7 +383,9 @@ struct RowSums {
 template <typename T, bool MASK, bool ONE, bool ONLY = false>
 __device__ __forceinline__ RowSums row_sums(RowShared &sh, const Row &row, const uint32_t *mask, int V, const Part &p, int wave, int nw, int lane, float c) {
     constexpr bool TWO = MASK && !ONLY;
-    const bool far = fabsf(p.top) < INFINITY && (fabsf(p.top * c) >= FAR_OFF || (TWO && ((p.seen && p.valid.s == 0.f) || (p.seen & LOST))));
+    // (+inf at a token that is not valid has raised a reference over valid ones: they are summed again, relative to the largest of themselves)
+    const bool far = TWO && p.top == INFINITY ? p.seen != 0u
+                                              : fabsf(p.top) < INFINITY && (fabsf(p.top * c) >= FAR_OFF || (TWO && ((p.seen && p.valid.s == 0.f) || (p.seen & LOST))));
     RowSums r;
     if (__builtin_expect(__builtin_amdgcn_readfirstlane(far), 0)) {   // (the same for all wavefronts of the row)
         take_row_careful<T, MASK>(row, mask, V, wave, nw, lane, c, r.all, r.q);

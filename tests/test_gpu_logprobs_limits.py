@@ -5,7 +5,7 @@ import torch
 
 from paper_2504_09135_amd import binding as ppv
 
-from gpu_helpers import DEV
+from gpu_helpers import DEV, to_dev, tuning
 from logprobs_oracle import Scores, check_values
 from test_gpu_logprobs import Case, hand_made_masks, tokens_for
 
@@ -41,3 +41,47 @@ def test_largest_and_smallest_temperatures(T, V, dtype):
                 want = Scores(c.x, v, c.tokens.cpu().numpy(), 1.0).top(40)[0]
                 assert np.array_equal(ids.cpu().numpy(), want)
                 check_values(lps.cpu().numpy(), np.where(want < 0, -np.inf, np.take_along_axis(c.ref.log_q, want.clip(0), 1)), "top_logprobs")
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,split", [(100, 0), (3001, 0), (40000, 0), (40000, 4), (150000, 0)])
+def test_infinities_and_nan_at_tokens_that_are_not_valid(V, split, dtype, value):
+    """What is not valid counts for log Z alone: the log probability, the entropy, the alternatives and the gradients of these are what
+    they are without it, and log Z says that there is none.  The odd token comes first, late, and more than once."""
+    rng = np.random.default_rng(V + split)
+    B = 16
+    x = rng.normal(0, 2.5, (B, V))
+    valid = hand_made_masks(B, V, rng)
+    valid[:, 5] = True
+    at = np.zeros((B, V), bool)
+    for b in range(B):
+        for v in (0, V // 2, V - 1)[:1 + b % 3][::-1 if b % 2 else 1]:
+            at[b, v] = True
+        at[b, rng.integers(0, V)] = True
+    at &= ~valid
+    assert at.any(1).sum() >= 8
+    tok = tokens_for(valid, B, V, rng)
+    with tuning(ppv.PPV_TUNE_ROW_SPLIT, split):
+        c = Case(x, dtype, valid, tok, T=0.8)
+        assert c.buf.shape[0] == B
+        c.logits[torch.from_numpy(at).to(DEV)] = value
+        lp, lz, h, st = c.forward()
+        torch.cuda.synchronize()
+        check_values(lp.cpu().numpy(), c.ref.logprobs, "logprobs")
+        check_values(h.cpu().numpy(), c.ref.entropy, "entropy")
+        odd = at.any(1) & (tok >= 0)
+        assert np.isnan(lz.cpu().numpy()[odd]).all()
+        check_values(lz.cpu().numpy()[~odd], c.ref.logZ[~odd], "logZ_valid")
+        for k in (3, 100):
+            c.check_top(k)
+        up = {n: u for n, u in c.up.items() if n != "d_logZ_valid"}
+        dev = {n: to_dev(u) for n, u in up.items()}
+        buf = c.gradient_buffer()
+        ppv.ppv_token_logprobs_backward(c.logits, c.tokens, st, buf[:, :V], mask=c.mask, temperature=c.T, **dev)
+        c.check_gradient(buf, up, "backward")
+        buf = c.gradient_buffer()
+        ppv.ppv_token_logprobs_grad(c.logits, c.tokens, buf[:, :V], lp, mask=c.mask, entropy=h, temperature=c.T, **dev)
+        c.check_gradient(buf, up, "grad")
+        check_values(lp.cpu().numpy(), c.ref.logprobs, "grad: logprobs")
+        check_values(h.cpu().numpy(), c.ref.entropy, "grad: entropy")
