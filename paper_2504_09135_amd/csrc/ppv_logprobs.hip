@@ -7,7 +7,8 @@
 //   entropy        = -sum q log q = log S - (sum y e^y) / S       with y = l - reference, S = sum e^y over the valid tokens
 //   d_l            = d_logprob (1[v = t] - q) + d_logZ (q - p) - d_entropy q (log q + entropy),   d_logits = d_l / T
 // A row is read once, by all lanes of its wavefronts, each with its own running reference and sums relative to it; the lanes' sums are
-// brought to one reference at the end.  Sums are fp32: a lane adds at most 4,096 terms of one sign.
+// brought to one reference at the end.  Sums are fp32.  A lane adds 16 or 32 terms a tile, 512 in all by the rules below (4,096
+// where one wavefront is asked for): those of s are of one sign, those of w, each times its exponent, below 0 but for tokens above the reference.
 #include <mutex>
 
 #include "ppv_rows.h"
@@ -46,9 +47,8 @@ __device__ __forceinline__ float uniform(float x) { return __int_as_float(__buil
 // An empty sum has a reference of LOWEST, which is finite: no difference below is that of two infinities.
 constexpr float FAR_OFF = 134217728.f;   // 2^27: below it the rounding of r is at most four units of the exponent
 constexpr float RAISE = 12.f;            // units of the exponent; entropies lose 12 * 2^-24 where a row's largest token comes late
-constexpr float FAINT_SUM = 9.09494702e-13f;   // 2^-40: valid tokens that weigh less than that against the lane's reference get one of their own
-constexpr float LOSING = 5.42101086e-20f;      // 2^-64: valid tokens that have come to weigh less, as the reference was raised, may be lost soon: the careful form again
-constexpr uint32_t LOST = 1u << 31;
+constexpr float FAINT_SUM = 0.00390625f;       // 2^-8: valid tokens that weigh less than that against most lanes' references get one of their own ...
+constexpr float LOST_SUM = 3.725290298461914e-9f;   // ... and 2^-28: those of one lane
 struct Run {
     float r, s, w;
 };
@@ -62,29 +62,38 @@ __device__ __forceinline__ Sums no_sums() { return {LOWEST, 0.f, 0.f}; }
 struct Tally {
     Run all;            // over all tokens (W without a mask: with w)
     float top, limit;   // the largest token; one above `limit` raises the reference
-    float s, w;         // with a mask: the valid tokens relative to all.r ...
+    Run valid;          // with a mask: the valid tokens relative to all.r as it was, or is ...
     Run few;            // ... and relative to a reference of their own
-    float few_top, few_limit;
-    uint32_t seen;      // bits of the mask; LOST
+    bool seen;          // bits of the mask
 };
-__device__ __forceinline__ Tally no_tally() { return {no_run(), -INFINITY, LOWEST, 0.f, 0.f, no_run(), -INFINITY, LOWEST, 0u}; }
+__device__ __forceinline__ Tally no_tally() { return {no_run(), -INFINITY, LOWEST, no_run(), no_run(), false}; }
 __device__ __forceinline__ void refer(float &s, float &w, float d) {   // to a reference that lies -d above
     const float f = fast_exp2(d);
     w = f * fmaf(d, s, w);
     s *= f;
 }
 __device__ __forceinline__ float reference_at(float top, float c) { return most(top * c, -FAR_OFF); }
-// The lane's reference is raised to its largest token where that lies above the limit (lanes whose does not: nothing changes).
-template <bool MASK> __device__ __forceinline__ void raise(Tally &a, float c, float step) {
+// Sums of valid tokens are brought together relative to what the heaviest of them weighs: not to the highest reference, which may be one that
+// the little there is lies far below, and by whose distance the others' exponents would be rounded.  (The sum of all has its reference's weight.)
+__device__ __forceinline__ float weight_of(const Run &a) { return a.s != 0.f ? a.r + fast_log2(a.s) : LOWEST; }
+template <bool W> __device__ __forceinline__ Run both(const Run &a, const Run &b) {
+    const float R = most(weight_of(a), weight_of(b)), da = most(a.r - R, FAINT), db = most(b.r - R, FAINT);
+    const float fa = a.s != 0.f ? fast_exp2(da) : 0.f, fb = b.s != 0.f ? fast_exp2(db) : 0.f;
+    return {R, fa * a.s + fb * b.s, W ? fa * fmaf(da, a.s, a.w) + fb * fmaf(db, b.s, b.w) : 0.f};
+}
+// A lane's valid tokens of the tile at hand, relative to the reference of all
+struct Weights {
+    float s, w;
+    bool some;   // bits of the mask
+};
+// The lane's reference is raised to its largest token where that lies above the limit (lanes whose does not: nothing changes).  IN: there are
+// valid tokens relative to it.
+template <bool IN> __device__ __forceinline__ void raise(Tally &a, Weights &in, float c, float step) {
     if (__ballot(a.top > a.limit) != 0ull) {
         const bool up = a.top > a.limit;
         const float r = up ? reference_at(a.top, c) : a.all.r, d = a.all.r - r;
         refer(a.all.s, a.all.w, d);
-        if (MASK) {
-            const bool some = a.s != 0.f;
-            refer(a.s, a.w, d);
-            a.seen |= some && a.s < LOSING ? LOST : 0u;
-        }
+        if (IN) refer(in.s, in.w, d);
         a.all.r = r;
         a.limit = up ? a.top + step : a.limit;
     }
@@ -103,52 +112,73 @@ __device__ __forceinline__ float if_bit(float x, uint32_t bits, int k) {
     return __uint_as_float((m & __float_as_uint(x)) | (~m & 0xFF800000u));   // x or -inf
 }
 // Valid tokens with a reference of their own
-template <int N, bool W> __device__ __forceinline__ void take_few(Tally &a, const float (&x)[N], float c, float step) {
-    a.few_top = N == 1 ? most(a.few_top, x[0]) : most_of<N>(x, a.few_top);
-    const bool up = a.few_top > a.few_limit;
+template <int N, bool W> __device__ __forceinline__ void take_few(Tally &a, const float (&x)[N], float c) {
+    const float top = N == 1 ? x[0] : most_of<N>(x, -INFINITY);
+    const bool up = fmaf(top, c, -a.few.r) > RAISE;   // (a limit, or the largest token so far, would take a register)
     if (__ballot(up) != 0ull) {
-        const float r = up ? reference_at(a.few_top, c) : a.few.r;
+        const float r = up ? reference_at(top, c) : a.few.r;
         refer(a.few.s, a.few.w, a.few.r - r);
         a.few.r = r;
-        a.few_limit = up ? a.few_top + step : a.few_limit;
     }
     add<N, W>(a.few, x, c);
 }
-// A group of a lane's tokens, `bits`: the valid ones.  Where few lanes have any, and where a lane's weigh too little against its reference, they
-// are left to be summed by themselves (true); else they are summed with the exponentials that are there.
+// A group of a lane's tokens, `bits`: the valid ones.  Where few lanes have any they are left to be summed by themselves (true); else they are
+// summed with the exponentials that are there.
 constexpr int FEW_LANES = 12;
-template <int N, bool MASK, bool W> __device__ __forceinline__ bool take_group(Tally &a, const float (&x)[N], uint32_t bits, float c, float step) {
+template <int N, bool MASK, bool W> __device__ __forceinline__ bool take_group(Tally &a, Weights &in, const float (&x)[N], uint32_t bits, float c, float step) {
     a.top = most_of<N>(x, a.top);
-    raise<MASK>(a, c, step);
-    if (MASK && __popcll(__ballot(bits != 0u)) > FEW_LANES) {
-        float s = 0.f, w = 0.f;
+    raise<MASK>(a, in, c, step);
+    const int lanes = MASK ? __popcll(__ballot(bits != 0u)) : 0;
+    if (lanes > FEW_LANES) {
 #pragma unroll
         for (int i = 0; i < N; i++) {
             const float y = fmaf(x[i], c, -a.all.r), e = fast_exp2(y);
             a.all.s += e;
             const float v = __uint_as_float(__float_as_uint(e) & all_ones_if(bits, i));
-            s += v;
-            if (W) w = fmaf(most(y, FAINT), v, w);
+            in.s += v;
+            if (W) in.w = fmaf(most(y, FAINT), v, in.w);
         }
-        const bool alone = s < FAINT_SUM;
-        a.s += alone ? 0.f : s;
-        if (W) a.w += alone ? 0.f : w;
-        return alone && bits != 0u;
+        in.some |= bits != 0u;
+        return false;
     }
     add<N, W && !MASK>(a.all, x, c);
-    return MASK && bits != 0u;
+    return lanes != 0;
+}
+// The tile's valid tokens join those before.  True: the lane's weigh too little against its reference, with those before, and are to be summed by
+// themselves.  That is so for all lanes where it is for most: where the model disagrees with a broad mask, the exponents of valid
+// tokens would be rounded as coarsely as they lie below the others', and an entropy is their mean.  (Half of V = 20,000 fp32 valid and lower by
+// 10 / 20 in the logits, entropies off by 4.2e-7 / 4.2e-7, root mean square, the plain form's 3.1e-7; by 9.8e-7 / 14.5e-7 where each lane
+// decides for itself, at 2^-40.  us so / now: scores of 1,024 rows at V = 256k bf16 under prefixes' masks 92.6 / 91.6, under broad ones 104.2 /
+// 101.3, 4,096 rows at V = 8k fp32 27.5 / 28.1; gradients of 64 rows at V = 32k 10.2 / 10.1, of 500 at V = 50k fp32 43.4 / 43.7.)
+template <bool W> __device__ __forceinline__ bool join(Tally &a, const Weights &in) {
+    const float d = a.valid.r - a.all.r;
+    if (__ballot(a.valid.s != 0.f && d != 0.f) != 0ull) {   // references have been raised
+        const Run before = a.valid;
+        refer(a.valid.s, a.valid.w, d);
+        const bool leave = a.valid.s < FAINT_SUM && before.s != 0.f;
+        if (__ballot(leave) != 0ull) {   // a sum that would weigh too little keeps the one it has, among the few
+            const Run few = both<W>(before, a.few);
+            a.few.r = leave ? few.r : a.few.r;
+            a.few.s = leave ? few.s : a.few.s;
+            a.few.w = leave ? few.w : a.few.w;
+            a.valid.s = leave ? 0.f : a.valid.s;
+            a.valid.w = leave ? 0.f : a.valid.w;
+        }
+    }
+    a.valid.r = a.all.r;
+    const float sum = a.valid.s + in.s;
+    const uint64_t some = __ballot(in.some), enough = __ballot(sum >= FAINT_SUM) & some;
+    const bool alone = in.some && sum < (2 * __popcll(enough) < __popcll(some) ? INFINITY : LOST_SUM);
+    a.valid.s = alone ? a.valid.s : sum;
+    if (W) a.valid.w += alone ? 0.f : in.w;
+    return alone;
 }
 
 template <typename T> __device__ __forceinline__ int tiles_in(int V) { return (V + TileGeom<T>::TILE - 1) / TileGeom<T>::TILE; }
 
-template <bool W> __device__ __forceinline__ Run over_lanes(const Run &a) {   // the wavefront's
-    const float r = a.s != 0.f ? a.r : LOWEST, R = wave_max(r), d = most(r - R, FAINT), f = fast_exp2(d);
+template <bool W, bool VALID> __device__ __forceinline__ Run over_lanes(const Run &a) {   // the wavefront's
+    const float R = wave_max(VALID ? weight_of(a) : (a.s != 0.f ? a.r : LOWEST)), d = most(a.r - R, FAINT), f = a.s != 0.f ? fast_exp2(d) : 0.f;
     return {R, wave_sum(f * a.s), W ? wave_sum(f * fmaf(d, a.s, a.w)) : 0.f};
-}
-template <bool W> __device__ __forceinline__ Run both(const Run &a, const Run &b) {
-    const float ra = a.s != 0.f ? a.r : LOWEST, rb = b.s != 0.f ? b.r : LOWEST, R = most(ra, rb);
-    const float da = most(ra - R, FAINT), db = most(rb - R, FAINT), fa = fast_exp2(da), fb = fast_exp2(db);
-    return {R, fa * a.s + fb * b.s, W ? fa * fmaf(da, a.s, a.w) + fb * fmaf(db, b.s, b.w) : 0.f};
 }
 // relative to a logit that makes the sum about 1: weights are then no smaller against it than they are.  (Any number will do.  At temperatures
 // near fp32's largest numbers that logit is outside them, or 1 / c infinite: the largest number, against which the sum is V at most.)
@@ -201,31 +231,36 @@ template <typename T> struct Gathered {
 template <typename T, bool MASK, bool W, bool PAD, bool FEW>
 __device__ __forceinline__ void take_groups(const MaskedTile<T, MASK> &mt, int left, int lane, float c, float step, Tally &a) {
     constexpr int EPL = Elem<T>::EPL;
-    uint32_t alone = 0u;   // the groups whose valid tokens are still to be summed
+    Weights in = {0.f, 0.f, false};
+    uint32_t left_over = 0u;   // the groups whose valid tokens are still to be summed
 #pragma unroll
     for (int j = 0; j < 4; j++) {
         float x[EPL];
         unpack_group<T, PAD>(mt.t.r[j], left - j * TileGeom<T>::PER_LOAD, x);
         if (FEW) {
             a.top = most_of<EPL>(x, a.top);
-            raise<true>(a, c, step);
+            raise<false>(a, in, c, step);
             add<EPL, false>(a.all, x, c);
         } else {
-            alone |= take_group<EPL, MASK, W>(a, x, mt.valid(j, lane), c, step) ? 1u << j : 0u;
+            left_over |= take_group<EPL, MASK, W>(a, in, x, mt.valid(j, lane), c, step) ? 1u << j : 0u;
         }
         __builtin_amdgcn_sched_barrier(0);   // one group's tokens in registers at a time
     }
-    if (!FEW && MASK && __ballot(alone != 0u) != 0ull) {
+    if (!FEW && MASK) {
+        const bool alone = join<W>(a, in);
+        if (__ballot(alone) != 0ull || left_over != 0u) {
 #pragma unroll 1
-        for (int j = 0; j < 4; j++) {
-            if (__ballot((alone >> j) & 1u) == 0ull) continue;
-            const u32x4 raw = j == 0 ? mt.t.r[0] : j == 1 ? mt.t.r[1] : j == 2 ? mt.t.r[2] : mt.t.r[3];
-            const uint32_t valid = mt.valid(j, lane), bits = (alone >> j) & 1u ? valid : 0u;   // (every lane takes part in the exchange)
-            float x[EPL];
-            unpack_group<T, PAD>(raw, left - j * TileGeom<T>::PER_LOAD, x);
+            for (int j = 0; j < 4; j++) {
+                const bool it = (left_over >> j) & 1u;
+                if (!it && __ballot(alone) == 0ull) continue;
+                const u32x4 raw = j == 0 ? mt.t.r[0] : j == 1 ? mt.t.r[1] : j == 2 ? mt.t.r[2] : mt.t.r[3];
+                const uint32_t valid = mt.valid(j, lane), bits = it || alone ? valid : 0u;   // (every lane takes part in the exchange)
+                float x[EPL];
+                unpack_group<T, PAD>(raw, left - j * TileGeom<T>::PER_LOAD, x);
 #pragma unroll
-            for (int i = 0; i < EPL; i++) x[i] = if_bit(x[i], bits, i);
-            take_few<EPL, W>(a, x, c, step);
+                for (int i = 0; i < EPL; i++) x[i] = if_bit(x[i], bits, i);
+                take_few<EPL, W>(a, x, c);
+            }
         }
     }
 }
@@ -234,7 +269,7 @@ __device__ __forceinline__ void take_tile(const Row &row, const MaskedTile<T, MA
     const int left = tokens_left<T>(V, tile, lane);
     const bool whole = (tile + 1) * TileGeom<T>::TILE <= V;
     const uint32_t w = MASK ? mt.t.word : 0u, w2 = w & (w - 1u);
-    if (MASK) a.seen |= w & ~LOST ? 1u : w >> 31;
+    if (MASK) a.seen |= w != 0u;
     if (MASK && __ballot((w2 & (w2 - 1u)) != 0u) == 0ull) {
         Gathered<T> g;
         g.load(row, w, tile, lane);
@@ -242,10 +277,10 @@ __device__ __forceinline__ void take_tile(const Row &row, const MaskedTile<T, MA
         else take_groups<T, MASK, W, true, true>(mt, left, lane, c, step, a);
         if (__ballot(w != 0u) != 0ull) {
             const float x0[1] = {w ? g.x[0] : -INFINITY};
-            take_few<1, W>(a, x0, c, step);
+            take_few<1, W>(a, x0, c);
             if (__ballot(w2 != 0u) != 0ull) {
                 const float x1[1] = {w2 ? g.x[1] : -INFINITY};
-                take_few<1, W>(a, x1, c, step);
+                take_few<1, W>(a, x1, c);
             }
         }
     } else {
@@ -308,11 +343,12 @@ __device__ __forceinline__ void take_row_careful(const Row &row, const uint32_t 
 struct Part {
     Run all, valid;   // over all tokens, and over the valid ones (TWO: they are told apart)
     float top;        // the largest token
-    uint32_t seen;    // 1: there were valid tokens; LOST
+    uint32_t seen;    // 1: there were valid tokens
 };
 template <bool TWO, bool W> __device__ __forceinline__ Part over_lanes(const Part &p) {
-    return {over_lanes<W && !TWO>(p.all), TWO ? over_lanes<W>(p.valid) : no_run(), wave_max(p.top),
-            TWO ? (__ballot(p.seen != 0u) ? 1u : 0u) | (__ballot(p.seen & LOST) ? LOST : 0u) : 0u};
+    const bool some = TWO && __ballot(p.valid.s != 0.f) != 0ull;
+    return {over_lanes<W && !TWO, false>(p.all), some ? over_lanes<W, true>(p.valid) : no_run(), wave_max(p.top),
+            TWO && __ballot(p.seen != 0u) != 0ull ? 1u : 0u};
 }
 __device__ __forceinline__ Part no_part() { return {no_run(), no_run(), -INFINITY, 0u}; }
 
@@ -326,7 +362,8 @@ struct RowShared {
 };
 // A workgroup's wavefronts' tallies and the token's logit (`x`: known to wavefront 0), to every wavefront.  ONE: there is one.
 template <bool TWO, bool W, bool ONE> __device__ __forceinline__ Part workgroup_part(RowShared &sh, const Tally &a, float &x, int wave, int nw, int lane) {
-    Part p = over_lanes<TWO, W>({a.all, TWO ? both<W>({a.all.r, a.s, a.w}, a.few) : no_run(), a.top, a.seen});
+    const Run valid = !TWO ? no_run() : __ballot(a.few.s != 0.f) != 0ull ? both<W>(a.valid, a.few) : a.valid;
+    Part p = over_lanes<TWO, W>({a.all, valid, a.top, a.seen ? 1u : 0u});
     if (ONE) return p;
     if (lane == 0) {
         sh.part[wave] = p;
@@ -385,7 +422,7 @@ __device__ __forceinline__ RowSums row_sums(RowShared &sh, const Row &row, const
     constexpr bool TWO = MASK && !ONLY;
     // (+inf at a token that is not valid has raised a reference over valid ones: they are summed again, relative to the largest of themselves)
     const bool far = TWO && p.top == INFINITY ? p.seen != 0u
-                                              : fabsf(p.top) < INFINITY && (fabsf(p.top * c) >= FAR_OFF || (TWO && ((p.seen && p.valid.s == 0.f) || (p.seen & LOST))));
+                                              : fabsf(p.top) < INFINITY && (fabsf(p.top * c) >= FAR_OFF || (TWO && p.seen && p.valid.s == 0.f));
     RowSums r;
     if (__builtin_expect(__builtin_amdgcn_readfirstlane(far), 0)) {   // (the same for all wavefronts of the row)
         take_row_careful<T, MASK>(row, mask, V, wave, nw, lane, c, r.all, r.q);
@@ -867,6 +904,7 @@ struct Best {
 template <typename T, bool MASK, bool W, bool PAD, bool HELD>
 __device__ __forceinline__ void top_tile_as(const MaskedTile<T, MASK> &mt, int i, int left, int lane, float c, float step, Tally &a, Best &best) {
     constexpr int EPL = Elem<T>::EPL;
+    Weights none;
 #pragma unroll
     for (int j = 0; j < 4; j++) {
         const uint32_t bits = mt.valid(j, lane);
@@ -879,7 +917,7 @@ __device__ __forceinline__ void top_tile_as(const MaskedTile<T, MASK> &mt, int i
         }
         const float g = most_of<EPL>(x, -INFINITY);
         a.top = most(a.top, g);
-        raise<false>(a, c, step);
+        raise<false>(a, none, c, step);
         add<EPL, W>(a.all, x, c);
         if (HELD) {
             best.third = __builtin_amdgcn_fmed3f(best.second, best.third, g);

@@ -85,3 +85,49 @@ def test_infinities_and_nan_at_tokens_that_are_not_valid(V, split, dtype, value)
         c.check_gradient(buf, up, "grad")
         check_values(lp.cpu().numpy(), c.ref.logprobs, "grad: logprobs")
         check_values(h.cpu().numpy(), c.ref.entropy, "grad: entropy")
+
+
+def plain_scores(x, valid, tok):
+    """log q_t and the entropy in fp32, relative to the largest valid token: differences, exponentials, sums."""
+    xv = torch.where(valid, x, -torch.inf)
+    m = xv.amax(1, keepdim=True)
+    y = xv - m
+    e = y.exp()
+    s = e.sum(1)
+    lp = y.gather(1, tok.long()[:, None])[:, 0] - s.log()
+    return lp, s.log() - torch.where(e > 0, y * e, 0.0).sum(1) / s
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [1000, 20000, 100003])
+@pytest.mark.parametrize("lower", [10.0, 20.0, 27.0])
+@pytest.mark.parametrize("where", ["everywhere", "first half"])
+def test_broad_valid_sets_of_little_mass(where, lower, V, dtype):
+    """A model that disagrees with a broad constraint, all over the row or after a part that it agrees with.  The valid tokens' exponents are rounded relative to what they lie below a reference:
+    where that is the valid tokens' own, as in the plain form, the errors are the plain form's but for the order of sums and for
+    references that lie up to 12 units of the exponent of 2 (8.3 of the logits) from the largest token; the plain form's exponents average
+    about 6 of the logits here (2.5 squared), so twice its error is room for either side."""
+    rng = np.random.default_rng(V + int(lower))
+    B = 200
+    x = rng.normal(0, 2.5, (B, V))
+    valid = rng.random((B, V)) < 0.5
+    if where == "first half":
+        valid[:, V // 2:] = False
+        x[:, V // 2:] += lower
+    else:
+        x -= lower * valid
+    tok = np.array([rng.choice(np.nonzero(v)[0]) for v in valid])
+    c = Case(x, dtype, valid, tok)
+    lp, lz, h, st = c.forward()
+    d = c.gradient_buffer()[:, :V]
+    lp2, h2 = torch.zeros(B, device=DEV), torch.zeros(B, device=DEV)
+    ppv.ppv_token_logprobs_grad(c.logits, c.tokens, d, lp2, mask=c.mask, entropy=h2, d_logprobs=torch.ones(B, device=DEV))
+    plain = plain_scores(c.logits.float(), torch.from_numpy(valid).to(DEV), c.tokens)
+    torch.cuda.synchronize()
+    rms = lambda got, want: float(np.sqrt(np.mean((got.double().cpu().numpy() - want) ** 2)))  # noqa: E731
+    for name, got, base, want in (("logprobs", lp, plain[0], c.ref.logprobs), ("entropy", h, plain[1], c.ref.entropy),
+                                  ("grad: logprobs", lp2, plain[0], c.ref.logprobs), ("grad: entropy", h2, plain[1], c.ref.entropy)):
+        ours, theirs = rms(got, want), rms(base, want)
+        print(f"{name}: {ours:.2e}, the plain form's {theirs:.2e}, {ours / theirs:.2f}")
+        assert ours <= 2 * theirs, (name, ours, theirs)
+    check_values(lz.cpu().numpy(), c.ref.logZ, "logZ_valid")
