@@ -1472,6 +1472,22 @@ ppv_status score_call(const Rows &rows, ppv_dtype dt, int B, const Area &area, c
 #undef PPV_CALL
     });
 }
+// Few rows of more tiles than this take two launches, the sums by several workgroups and then the gradient; others one, where a workgroup has all
+// of a row's sums and reads again what it cannot hold.  Many parts gain most (up to 64 rows are split into four or more, then into two), and more
+// under masks, whose sums take longer.  us in one launch / in two, random masks of a tenth in every eighth row:
+//   fp32    32 rows  60 tiles 10.5 / 10.3, 65 13.5 / 11.1, 250 59.8 / 21.4;  64 rows  60 tiles 11.3 / 12.6, 65 14.5 / 13.9
+//           96 rows  80 tiles 21.9 / 21.8, 88 24.7 / 23.0;  128 rows  98 tiles 30.0 / 31.6, 110 35.3 / 35.8, 128 42.3 / 40.8
+//   masked  32 rows  36 tiles 12.6 / 12.4, 42 13.4 / 12.4;  64 rows  36 tiles 13.2 / 13.3, 42 14.3 / 13.4, 98 32.1 / 21.0
+//           96 rows  60 tiles 18.7 / 18.8, 65 24.0 / 20.5;  128 rows  60 tiles 19.3 / 23.7, 65 26.3 / 25.2
+//   bf16    32 rows  36 tiles 10.9 / 11.2, 44 12.1 / 11.0;  64 rows  40 tiles 11.9 / 11.7, 44 13.0 / 12.0, 128 42.1 / 24.6
+//           96 rows  56 tiles 18.1 / 17.9, 60 18.9 / 18.2;  128 rows  80 tiles 28.3 / 28.7, 90 32.4 / 32.4, 105 38.0 / 36.5
+//   masked   4 rows  27 tiles 12.5 / 12.7, 29 14.0 / 12.8;  64 rows  24 tiles 12.3 / 13.5, 27 14.1 / 13.4, 29 15.9 / 13.4
+//           96 rows  32 tiles 18.2 / 14.8;  128 rows  32 tiles 18.3 / 16.1  (fewer are not split)
+int tiles_of_one_launch(ppv_dtype dt, bool masked, int B) {
+    const int rows = B <= 64 ? 0 : (B <= 96 ? 1 : 2);
+    static constexpr int MOST[2][2][3] = {{{64, 84, 112}, {40, 64, 64}}, {{40, 56, 88}, {27, 31, 31}}};   // fp32, bf16; without a mask, under one
+    return MOST[dt == PPV_F32 ? 0 : 1][masked ? 1 : 0][rows];
+}
 ppv_status gradient_call(const Rows &rows, ppv_dtype dt, int B, const float *stats, void *d_logits, int64_t d_stride, const Upstream &up, const Temper &tp) {
     Shape sh = shape_of(rows.V, dt, B);
     // No wavefront waits for another here.  us with 4 / 8 / 16 wavefronts, bf16: V = 32k, 64 rows 4.7 / 4.9 / 6.6, 2,048 rows 51.5 / 49.5 / 46.7;
@@ -1539,11 +1555,7 @@ extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, 
     int nw = (int)sh.block / WAVE;
     while (!sh.one && nw < MOST_WAVES && nt > MOST_HELD * nw) nw *= 2;   // enough wavefronts to hold the row, if there are as many
     const int held = (nt + nw - 1) / nw;
-    // Few rows that no workgroup can hold, or not without long work on their masks: the sums by several workgroups, then the gradient.  (us
-    // in one launch / in two: V = 100k fp32 32 rows 20.9 / 12.1, 128 rows 28.4 / 31.5, masked 30.1 / 13.8, 36.5 / 34.4; V = 256k bf16 36.7 / 14.1,
-    // 43.1 / 40.0; V = 100k bf16 masked 20.6 / 12.6, 25.8 / 24.2, but 32 rows without a mask, V = 128k 16.2 / 16.2, and masked, V = 64k 14.5 / 14.2,
-    // V = 50k fp32 15.6 / 16.3.)
-    if (held > MOST_HELD || (mask && V >= 96000)) {
+    if (nt > tiles_of_one_launch(dt, mask != nullptr, B)) {
         const Area area = area_for(V, dt, B, 0, PPV_SPLIT_MAX_PARTS, (hipStream_t)stream);
         if (area.shift) {
             static std::mutex both;   // another thread's call on this stream does not come between the two launches
