@@ -1,4 +1,5 @@
-"""The calls on given tokens at the limits of what they take."""
+"""The calls on given tokens at the limits of what they take: the largest and smallest temperatures, infinities and NaN at tokens that are
+not valid, valid tokens of little mass, gradients over the logits of rows that are summed twice, eager calls beside a graph that runs."""
 import numpy as np
 import pytest
 import torch
@@ -7,7 +8,7 @@ from paper_2504_09135_amd import binding as ppv
 
 from gpu_helpers import DEV, to_dev, tuning
 from logprobs_oracle import Scores, check_values
-from test_gpu_logprobs import Case, hand_made_masks, tokens_for
+from test_gpu_logprobs import Case, hand_made_masks, odd_values, tokens_for
 
 pytestmark = pytest.mark.gpu
 
@@ -131,3 +132,88 @@ def test_broad_valid_sets_of_little_mass(where, lower, V, dtype):
         print(f"{name}: {ours:.2e}, the plain form's {theirs:.2e}, {ours / theirs:.2f}")
         assert ours <= 2 * theirs, (name, ours, theirs)
     check_values(lz.cpu().numpy(), c.ref.logZ, "logZ_valid")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [100, 3001, 40000, 140001])
+@pytest.mark.parametrize("kind", ["far", "lowest", "late peak", "low mass", "stairs", "high"])
+def test_gradient_in_place_of_rows_that_are_summed_twice(kind, V, dtype):
+    """d_logits may be the logits themselves also where the sums are taken again, by every wavefront from all of the row: none of them writes
+    before all have read."""
+    rng = np.random.default_rng(V)
+    B = 10
+    x = odd_values(kind, B, V, rng)
+    valid = hand_made_masks(B, V, rng)
+    if kind == "low mass":
+        valid[:, :V // 2] = False
+    if kind == "late peak":
+        valid[:, V // 2:] = False
+    if kind == "stairs":
+        valid[:, V // 9:] = False
+    for v in (None, valid):
+        c = Case(x, dtype, v, tokens_for(v, B, V, rng))
+        dev = {n: to_dev(u) for n, u in c.up.items()}
+        lp, h = torch.zeros(B, device=DEV), torch.zeros(B, device=DEV)
+        ppv.ppv_token_logprobs_grad(c.logits, c.tokens, c.logits, lp, mask=c.mask, entropy=h, temperature=c.T, **dev)
+        c.check_gradient(c.buf, c.up, kind + " in place")
+        check_values(lp.cpu().numpy(), c.ref.logprobs, kind)
+        check_values(h.cpu().numpy(), c.ref.entropy, kind)
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_eager_calls_beside_a_graph_that_runs(masked):
+    """A graph's calls and eager ones on another stream, queued together, so that they may run at the same time: split rows and calls of two
+    launches meet in areas of their own.  The results of both are those of calls alone, to the bit."""
+    rng = np.random.default_rng(20)
+    B, V, K = 5, 200003, 7
+    valid = hand_made_masks(B, V, rng) if masked else None
+    cases = [Case(rng.normal(0, 2, (B, V)), "bf16", valid, tokens_for(valid, B, V, rng), seed=i) for i in range(2)]
+    f = lambda *s, **kw: torch.zeros(s, device=DEV, **kw)  # noqa: E731
+
+    class Set:
+        def __init__(self, c):
+            self.c, self.up = c, {n: to_dev(u) for n, u in c.up.items()}
+            self.outs = [f(B), f(B), f(B), f(B, ppv.PPV_LOGPROB_STATS), f(B), f(B, K, dtype=torch.int32), f(B, K)]
+            self.d = c.gradient_buffer()
+
+        def calls(self, stream=None):
+            lp, lz, h, st, lp2, ids, lps = self.outs
+            c = self.c
+            ppv.ppv_token_logprobs(c.logits, c.tokens, lp, mask=c.mask, logZ_valid=lz, entropy=h, stats=st, stream=stream)
+            ppv.ppv_token_logprobs_grad(c.logits, c.tokens, self.d[:, :V], lp2, mask=c.mask, stream=stream, **self.up)
+            ppv.ppv_top_logprobs(c.logits, K, ids, lps, mask=c.mask, stream=stream)
+
+        def clear(self):
+            for t in self.outs:
+                t.fill_(9)
+            self.d[:, :V] = 9
+
+        def results(self):
+            return [t.clone() for t in (*self.outs, self.d)]
+
+    sets = [Set(c) for c in cases]
+    other = torch.cuda.Stream()
+    for s in sets:      # (areas are laid ready)
+        s.calls()
+        s.calls(other)
+    torch.cuda.synchronize()
+    alone = [s.results() for s in sets]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(4):
+            sets[0].calls()
+    for _ in range(5):
+        for s in sets:
+            s.clear()
+        torch.cuda.synchronize()
+        graph.replay()
+        for _ in range(4):
+            sets[1].calls(other)
+        graph.replay()
+        torch.cuda.synchronize()
+        for s, want in zip(sets, alone):
+            for a, b in zip(s.results(), want):
+                assert torch.equal(a, b)
+    for s in sets:
+        check_values(s.outs[0].cpu().numpy(), s.c.ref.logprobs, "logprobs")
+        assert np.array_equal(s.outs[5].cpu().numpy(), Scores(s.c.x, valid, None, 1.0).top(K)[0])
