@@ -87,15 +87,16 @@ struct Weights {
     bool some;   // bits of the mask
 };
 // The lane's reference is raised to its largest token where that lies above the limit (lanes whose does not: nothing changes).  IN: there are
-// valid tokens relative to it.
+// valid tokens relative to it.  A largest token of NaN, which one that signals among the others makes (quiet ones are passed over), counts as +inf.
 template <bool IN> __device__ __forceinline__ void raise(Tally &a, Weights &in, float c, float step) {
-    if (__ballot(a.top > a.limit) != 0ull) {
+    if (__ballot(!(a.top <= a.limit)) != 0ull) {
         const bool up = a.top > a.limit;
         const float r = up ? reference_at(a.top, c) : a.all.r, d = a.all.r - r;
         refer(a.all.s, a.all.w, d);
         if (IN) refer(in.s, in.w, d);
         a.all.r = r;
         a.limit = up ? a.top + step : a.limit;
+        a.top = a.top != a.top ? INFINITY : a.top;
     }
 }
 template <int N, bool W> __device__ __forceinline__ void add(Run &a, const float (&x)[N], float c) {
@@ -420,7 +421,7 @@ struct RowSums {
 template <typename T, bool MASK, bool ONE, bool ONLY = false>
 __device__ __forceinline__ RowSums row_sums(RowShared &sh, const Row &row, const uint32_t *mask, int V, const Part &p, int wave, int nw, int lane, float c) {
     constexpr bool TWO = MASK && !ONLY;
-    // (+inf at a token that is not valid has raised a reference over valid ones: they are summed again, relative to the largest of themselves)
+    // (+inf or NaN at a token that is not valid has raised a reference over valid ones: they are summed again, relative to the largest of themselves)
     const bool far = TWO && p.top == INFINITY ? p.seen != 0u
                                               : fabsf(p.top) < INFINITY && (fabsf(p.top * c) >= FAR_OFF || (TWO && p.seen && p.valid.s == 0.f));
     RowSums r;

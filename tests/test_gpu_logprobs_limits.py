@@ -44,7 +44,11 @@ def test_largest_and_smallest_temperatures(T, V, dtype):
                 check_values(lps.cpu().numpy(), np.where(want < 0, -np.inf, np.take_along_axis(c.ref.log_q, want.clip(0), 1)), "top_logprobs")
 
 
-@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+# a NaN that signals, as memory that nobody has written may hold; one of the other sign
+BITS = {"signalling": {"f32": 0x7F800001, "bf16": 0x7F81}, "negative": {"f32": -1, "bf16": -1}}
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("nan"), "signalling", "negative"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V,split", [(100, 0), (3001, 0), (40000, 0), (40000, 4), (150000, 0)])
 def test_infinities_and_nan_at_tokens_that_are_not_valid(V, split, dtype, value):
@@ -66,7 +70,10 @@ def test_infinities_and_nan_at_tokens_that_are_not_valid(V, split, dtype, value)
     with tuning(ppv.PPV_TUNE_ROW_SPLIT, split):
         c = Case(x, dtype, valid, tok, T=0.8)
         assert c.buf.shape[0] == B
-        c.logits[torch.from_numpy(at).to(DEV)] = value
+        if value in BITS:
+            c.logits.view(torch.int32 if dtype == "f32" else torch.int16)[torch.from_numpy(at).to(DEV)] = BITS[value][dtype]
+        else:
+            c.logits[torch.from_numpy(at).to(DEV)] = value
         lp, lz, h, st = c.forward()
         torch.cuda.synchronize()
         check_values(lp.cpu().numpy(), c.ref.logprobs, "logprobs")
