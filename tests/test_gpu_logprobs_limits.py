@@ -7,7 +7,7 @@ import torch
 from paper_2504_09135_amd import binding as ppv
 
 from gpu_helpers import DEV, to_dev, tuning
-from logprobs_oracle import Scores, check_values
+from logprobs_oracle import Scores, check_gradient, check_values, unpack
 from test_gpu_logprobs import Case, hand_made_masks, odd_values, tokens_for
 
 pytestmark = pytest.mark.gpu
@@ -224,3 +224,35 @@ def test_eager_calls_beside_a_graph_that_runs(masked):
     for s in sets:
         check_values(s.outs[0].cpu().numpy(), s.c.ref.logprobs, "logprobs")
         assert np.array_equal(s.outs[5].cpu().numpy(), Scores(s.c.x, valid, None, 1.0).top(K)[0])
+
+
+@pytest.mark.parametrize("V,dtype", [(9, "f32"), (70, "bf16"), (1030, "f32")])
+def test_more_rows_than_a_launch_takes(V, dtype):
+    """2^21 rows and some: the rows behind are another launch's, with their own tokens, masks, gradients and results."""
+    B, per = (1 << 21) + 5, 4 if dtype == "f32" else 8
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    g = torch.Generator(device=DEV).manual_seed(V)
+    x = torch.empty((B, (V + per - 1) // per * per), dtype=dt, device=DEV).normal_(0, 2, generator=g)[:, :V]
+    mask = torch.randint(-(1 << 31), (1 << 31) - 1, (B, (V + 31) // 32), generator=g, device=DEV, dtype=torch.int32)
+    if V % 32:
+        mask[:, -1] &= (1 << V % 32) - 1
+    tokens = torch.randint(0, V, (B,), generator=g, device=DEV).to(torch.int32)
+    lp, lz, h, up = (torch.randn((B,), generator=g, device=DEV) for _ in range(4))
+    lp2, ids, lps = torch.zeros(B, device=DEV), torch.zeros((B, 3), dtype=torch.int32, device=DEV), torch.zeros((B, 3), device=DEV)
+    stats = torch.zeros((B, ppv.PPV_LOGPROB_STATS), device=DEV)
+    rows = torch.tensor([0, 1, 4_095, (1 << 21) - 1, *range(1 << 21, B)], device=DEV)
+    ref = Scores(x[rows].double().cpu().numpy(), unpack(mask[rows].cpu().numpy(), V), tokens[rows].cpu().numpy(), 1.0)
+    want, size = ref.gradient(up[rows].cpu().numpy(), None, None)
+    ppv.ppv_token_logprobs(x, tokens, lp, mask=mask, logZ_valid=lz, entropy=h, stats=stats)
+    ppv.ppv_top_logprobs(x, 3, ids, lps, mask=mask)
+    d = torch.zeros((B, x.stride(0)), dtype=dt, device=DEV)[:, :V]
+    ppv.ppv_token_logprobs_backward(x, tokens, stats, d, mask=mask, d_logprobs=up)
+    check_values(lp[rows].cpu().numpy(), ref.logprobs, "logprobs")
+    check_values(lz[rows].cpu().numpy(), ref.logZ, "logZ_valid")
+    check_values(h[rows].cpu().numpy(), ref.entropy, "entropy")
+    assert np.array_equal(ids[rows].cpu().numpy(), ref.top(3)[0])
+    check_values(lps[rows].cpu().numpy(), ref.top(3)[1], "top_logprobs")
+    check_gradient(d[rows].float().cpu().numpy(), want, size, dtype, "backward")
+    ppv.ppv_token_logprobs_grad(x, tokens, x, lp2, mask=mask, d_logprobs=up)       # in place
+    check_gradient(x[rows].float().cpu().numpy(), want, size, dtype, "grad")
+    check_values(lp2[rows].cpu().numpy(), ref.logprobs, "grad: logprobs")
