@@ -150,14 +150,14 @@ template <int N, bool MASK, bool W> __device__ __forceinline__ bool take_group(T
 // tokens would be rounded as coarsely as they lie below the others', and an entropy is their mean.  (Half of V = 20,000 fp32 valid and lower by
 // 10 / 20 in the logits, entropies off by 4.2e-7 / 4.2e-7, root mean square, the plain form's 3.1e-7; by 9.8e-7 / 14.5e-7 where each lane
 // decides for itself, at 2^-40.  us so / now: scores of 1,024 rows at V = 256k bf16 under prefixes' masks 92.6 / 91.6, under broad ones 104.2 /
-// 101.3, 4,096 rows at V = 8k fp32 27.5 / 28.1; gradients of 64 rows at V = 32k 10.2 / 10.1, of 500 at V = 50k fp32 43.4 / 43.7.)
+// 101.3, 4,096 rows at V = 8k fp32 27.5 / 28.2; gradients of 64 rows at V = 32k 10.1 / 10.2, of 500 at V = 50k fp32 42.8 / 43.1.)
 template <bool W> __device__ __forceinline__ bool join(Tally &a, const Weights &in) {
     const float d = a.valid.r - a.all.r;
     if (__ballot(a.valid.s != 0.f && d != 0.f) != 0ull) {   // references have been raised
         const Run before = a.valid;
         refer(a.valid.s, a.valid.w, d);
-        const bool leave = a.valid.s < FAINT_SUM && before.s != 0.f;
-        if (__ballot(leave) != 0ull) {   // a sum that would weigh too little keeps the one it has, among the few
+        const bool leave = a.valid.s < LOST_SUM && before.s != 0.f;
+        if (__ballot(leave) != 0ull) {   // a sum that would weigh too little keeps the one it has, among the few.  (Others are rounded once by the distance.)
             const Run few = both<W>(before, a.few);
             a.few.r = leave ? few.r : a.few.r;
             a.few.s = leave ? few.s : a.few.s;
