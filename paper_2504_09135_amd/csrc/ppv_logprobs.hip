@@ -75,10 +75,10 @@ __device__ __forceinline__ void refer(float &s, float &w, float d) {   // to a r
 __device__ __forceinline__ float reference_at(float top, float c) { return most(top * c, -FAR_OFF); }
 // Sums of valid tokens are brought together relative to what the heaviest of them weighs: not to the highest reference, which may be one that
 // the little there is lies far below, and by whose distance the others' exponents would be rounded.  (The sum of all has its reference's weight.)
-__device__ __forceinline__ float weight_of(const Run &a) { return a.s != 0.f ? a.r + fast_log2(a.s) : LOWEST; }
+__device__ __forceinline__ float weight_of(const Run &a, float r) { return r + (a.s != 0.f ? fast_log2(a.s) : 0.f); }
 template <bool W> __device__ __forceinline__ Run both(const Run &a, const Run &b) {
-    const float R = most(weight_of(a), weight_of(b)), da = most(a.r - R, FAINT), db = most(b.r - R, FAINT);
-    const float fa = a.s != 0.f ? fast_exp2(da) : 0.f, fb = b.s != 0.f ? fast_exp2(db) : 0.f;
+    const float ra = a.s != 0.f ? a.r : LOWEST, rb = b.s != 0.f ? b.r : LOWEST, R = most(weight_of(a, ra), weight_of(b, rb));
+    const float da = most(ra - R, FAINT), db = most(rb - R, FAINT), fa = fast_exp2(da), fb = fast_exp2(db);
     return {R, fa * a.s + fb * b.s, W ? fa * fmaf(da, a.s, a.w) + fb * fmaf(db, b.s, b.w) : 0.f};
 }
 // A lane's valid tokens of the tile at hand, relative to the reference of all
@@ -88,15 +88,15 @@ struct Weights {
 };
 // The lane's reference is raised to its largest token where that lies above the limit (lanes whose does not: nothing changes).  IN: there are
 // valid tokens relative to it.  A largest token of NaN, which one that signals among the others makes (quiet ones are passed over), counts as +inf.
-template <bool IN> __device__ __forceinline__ void raise(Tally &a, Weights &in, float c, float step) {
-    if (__ballot(!(a.top <= a.limit)) != 0ull) {
+template <bool MASK, bool IN> __device__ __forceinline__ void raise(Tally &a, Weights &in, float c, float step) {
+    if (__ballot(MASK ? !(a.top <= a.limit) : a.top > a.limit) != 0ull) {
         const bool up = a.top > a.limit;
         const float r = up ? reference_at(a.top, c) : a.all.r, d = a.all.r - r;
         refer(a.all.s, a.all.w, d);
         if (IN) refer(in.s, in.w, d);
         a.all.r = r;
         a.limit = up ? a.top + step : a.limit;
-        a.top = a.top != a.top ? INFINITY : a.top;
+        if (MASK) a.top = a.top != a.top ? INFINITY : a.top;
     }
 }
 template <int N, bool W> __device__ __forceinline__ void add(Run &a, const float (&x)[N], float c) {
@@ -128,7 +128,7 @@ template <int N, bool W> __device__ __forceinline__ void take_few(Tally &a, cons
 constexpr int FEW_LANES = 12;
 template <int N, bool MASK, bool W> __device__ __forceinline__ bool take_group(Tally &a, Weights &in, const float (&x)[N], uint32_t bits, float c, float step) {
     a.top = most_of<N>(x, a.top);
-    raise<MASK>(a, in, c, step);
+    raise<MASK, MASK>(a, in, c, step);
     const int lanes = MASK ? __popcll(__ballot(bits != 0u)) : 0;
     if (lanes > FEW_LANES) {
 #pragma unroll
@@ -178,14 +178,14 @@ template <bool W> __device__ __forceinline__ bool join(Tally &a, const Weights &
 template <typename T> __device__ __forceinline__ int tiles_in(int V) { return (V + TileGeom<T>::TILE - 1) / TileGeom<T>::TILE; }
 
 template <bool W, bool VALID> __device__ __forceinline__ Run over_lanes(const Run &a) {   // the wavefront's
-    const float R = wave_max(VALID ? weight_of(a) : (a.s != 0.f ? a.r : LOWEST)), d = most(a.r - R, FAINT), f = a.s != 0.f ? fast_exp2(d) : 0.f;
+    const float r = a.s != 0.f ? a.r : LOWEST, R = wave_max(VALID ? weight_of(a, r) : r), d = most(r - R, FAINT), f = fast_exp2(d);
     return {R, wave_sum(f * a.s), W ? wave_sum(f * fmaf(d, a.s, a.w)) : 0.f};
 }
 // relative to a logit that makes the sum about 1: weights are then no smaller against it than they are.  (Any number will do.  At temperatures
 // near fp32's largest numbers that logit is outside them, or 1 / c infinite: the largest number, against which the sum is V at most.)
 __device__ __forceinline__ Sums sums_of(const Run &a, float c) {
     if (!(a.s != 0.f)) return no_sums();
-    const float m = most(fminf((a.r + fast_log2(a.s)) * __builtin_amdgcn_rcpf(c), -LOWEST), LOWEST), d = fmaf(-m, c, a.r), f = fast_exp2(d);
+    const float m = __builtin_amdgcn_fmed3f((a.r + fast_log2(a.s)) * __builtin_amdgcn_rcpf(c), LOWEST, -LOWEST), d = fmaf(-m, c, a.r), f = fast_exp2(d);
     return {m, f * a.s, f * fmaf(d, a.s, a.w)};
 }
 
@@ -240,7 +240,7 @@ __device__ __forceinline__ void take_groups(const MaskedTile<T, MASK> &mt, int l
         unpack_group<T, PAD>(mt.t.r[j], left - j * TileGeom<T>::PER_LOAD, x);
         if (FEW) {
             a.top = most_of<EPL>(x, a.top);
-            raise<false>(a, in, c, step);
+            raise<true, false>(a, in, c, step);
             add<EPL, false>(a.all, x, c);
         } else {
             left_over |= take_group<EPL, MASK, W>(a, in, x, mt.valid(j, lane), c, step) ? 1u << j : 0u;
@@ -458,7 +458,7 @@ struct RowValues {
     float logprob, logZ, entropy;
 };
 // (a - b) / T + more; the difference may be outside fp32 where this is not
-__device__ __forceinline__ float over_t(float a, float b, const Temper &tp, float more) { return 2.f * fmaf(0.5f * a - 0.5f * b, tp.inv, 0.5f * more); }
+__device__ __forceinline__ float over_t(float a, float b, const Temper &tp, float more) { return 2.f * fmaf(fmaf(-0.5f, b, 0.5f * a), tp.inv, 0.5f * more); }
 // what the sums say.  Without mass (no valid token, or all at -inf): -inf, and an entropy of 0.
 template <bool MASK> __device__ __forceinline__ RowValues row_values(const Sums &all, const Sums &q, float x, const Temper &tp, float log_s) {
     if (!(q.s != 0.f)) return {-INFINITY, -INFINITY, 0.f};
@@ -918,7 +918,7 @@ __device__ __forceinline__ void top_tile_as(const MaskedTile<T, MASK> &mt, int i
         }
         const float g = most_of<EPL>(x, -INFINITY);
         a.top = most(a.top, g);
-        raise<false>(a, none, c, step);
+        raise<false, false>(a, none, c, step);
         add<EPL, W>(a.all, x, c);
         if (HELD) {
             best.third = __builtin_amdgcn_fmed3f(best.second, best.third, g);
