@@ -1474,19 +1474,19 @@ ppv_status score_call(const Rows &rows, ppv_dtype dt, int B, const Area &area, c
     });
 }
 // Few rows of more tiles than this take two launches, the sums by several workgroups and then the gradient; others one, where a workgroup has all
-// of a row's sums and reads again what it cannot hold.  Many parts gain most (up to 64 rows are split into four or more, then into two), and more
-// under masks, whose sums take longer.  us in one launch / in two, random masks of a tenth in every eighth row:
-//   fp32    32 rows  60 tiles 10.5 / 10.3, 65 13.5 / 11.1, 250 59.8 / 21.4;  64 rows  60 tiles 11.3 / 12.6, 65 14.5 / 13.9
+// of a row's sums and reads again what it cannot hold (of more than 64 tiles).  Many parts gain most (up to 64 rows are split into four or more,
+// then into two), and more under masks, whose sums take longer.  us in one launch / in two, masks as prefixes have them:
+//   fp32    32 rows  56 tiles 10.4 / 10.3, 65 13.5 / 11.1, 250 59.8 / 21.4;  64 rows  60 tiles 11.2 / 12.4, 63 11.7 / 12.5, 65 14.5 / 13.9
 //           96 rows  80 tiles 21.9 / 21.8, 88 24.7 / 23.0;  128 rows  98 tiles 30.0 / 31.6, 110 35.3 / 35.8, 128 42.3 / 40.8
-//   masked  32 rows  36 tiles 12.6 / 12.4, 42 13.4 / 12.4;  64 rows  36 tiles 13.2 / 13.3, 42 14.3 / 13.4, 98 32.1 / 21.0
-//           96 rows  60 tiles 18.7 / 18.8, 65 24.0 / 20.5;  128 rows  60 tiles 19.3 / 23.7, 65 26.3 / 25.2
-//   bf16    32 rows  36 tiles 10.9 / 11.2, 44 12.1 / 11.0;  64 rows  40 tiles 11.9 / 11.7, 44 13.0 / 12.0, 128 42.1 / 24.6
-//           96 rows  56 tiles 18.1 / 17.9, 60 18.9 / 18.2;  128 rows  80 tiles 28.3 / 28.7, 90 32.4 / 32.4, 105 38.0 / 36.5
-//   masked   4 rows  27 tiles 12.5 / 12.7, 29 14.0 / 12.8;  64 rows  24 tiles 12.3 / 13.5, 27 14.1 / 13.4, 29 15.9 / 13.4
-//           96 rows  32 tiles 18.2 / 14.8;  128 rows  32 tiles 18.3 / 16.1  (fewer are not split)
+//   masked  32 rows  36 tiles 12.7 / 12.5, 42 13.4 / 12.3;  64 rows  36 tiles 13.1 / 13.1, 39 13.3 / 13.2, 42 14.1 / 13.2, 98 32.1 / 21.0
+//           96 rows  60 tiles 17.8 / 18.7, 63 19.4 / 19.1, 65 24.0 / 20.5;  128 rows  63 tiles 20.1 / 23.8, 65 26.3 / 25.2
+//   bf16    32 rows  36 tiles 10.8 / 10.9, 40 11.5 / 11.0;  64 rows  36 tiles 11.2 / 11.6, 40 11.9 / 11.6, 128 42.1 / 24.6
+//           96 rows  63 tiles 17.5 / 18.2, 65 21.5 / 19.8;  128 rows  80 tiles 28.3 / 28.7, 90 32.4 / 32.4, 105 38.0 / 36.5
+//   masked   4 rows  27 tiles 12.5 / 12.5, broad masks 12.5 / 13.0, 29 13.6 / 12.3, 14.3 / 12.9;  64 rows  27 tiles 13.6 / 13.2, 13.6 / 13.6, 29 15.3 / 13.1
+//           96 rows  32 tiles 16.3 / 14.5, 48 21.6 / 20.2 (fewer are not split);  128 rows  32 tiles 16.4 / 15.9, 40 18.2 / 20.3, 65 32.9 / 28.2
 int tiles_of_one_launch(ppv_dtype dt, bool masked, int B) {
     const int rows = B <= 64 ? 0 : (B <= 96 ? 1 : 2);
-    static constexpr int MOST[2][2][3] = {{{64, 84, 112}, {40, 64, 64}}, {{40, 56, 88}, {27, 31, 31}}};   // fp32, bf16; without a mask, under one
+    static constexpr int MOST[2][2][3] = {{{64, 84, 112}, {38, 62, 64}}, {{39, 64, 88}, {27, 31, 64}}};   // fp32, bf16; without a mask, under one
     return MOST[dt == PPV_F32 ? 0 : 1][masked ? 1 : 0][rows];
 }
 ppv_status gradient_call(const Rows &rows, ppv_dtype dt, int B, const float *stats, void *d_logits, int64_t d_stride, const Upstream &up, const Temper &tp) {
@@ -1567,11 +1567,11 @@ extern "C" ppv_status ppv_token_logprobs_grad(const void *logits, ppv_dtype dt, 
             return gradient_call(rows, dt, B, out.stats, d_logits, d_row_stride, up, tp);
         }
     }
-    // Two or four workgroups to a row of a small batch.  (us with one / two / four, V = 32k bf16 masked: 32 rows 11.1 / 10.0 / 9.6, 64 rows 11.1 /
-    // 10.2 / 10.3, 128 rows 11.3 / 10.9 / 17.6; without masks 7.8 / 7.2 / 7.1, 8.1 / 7.4 / 7.6, 8.1 / 8.1 / 13.0.)  They read the whole
-    // row: not where another one writes it.
+    // Two or four workgroups to a row of a small batch, up to one to a compute unit.  (us with one / two / four, V = 32k bf16 masked: 32 rows 11.2 / 10.0 /
+    // 9.6, 64 rows 11.3 / 10.1 / 9.7, 128 rows 11.4 / 10.3 / 16.7; without masks 8.0 / 7.2 / 6.9, 8.3 / 7.5 / 7.2, 8.2 / 7.6 / 11.8; V = 50k fp32 64 rows
+    // 11.1 / 9.9 / 9.7, 96 rows 11.2 / 10.2 / 18.2.)  They read the whole row: not where another one writes it.
     int shift = 0;
-    while (!sh.one && held <= MOST_HELD && d_logits != logits && shift < 2 && nt >= 8 && (int64_t)B << (shift + 1) <= 128) shift++;
+    while (!sh.one && held <= MOST_HELD && d_logits != logits && shift < 2 && nt >= 8 && (int64_t)B << (shift + 1) <= 256) shift++;
     if (!sh.one) sh.block = (unsigned)nw * WAVE;
     return in_turns(rows, B, [&](const Rows &r) {
 #define PPV_CALL(T, MASK, W) launch_score_gradient<T, MASK, W>(r, sh, held, shift, d_logits, d_row_stride, out, up, tp)
